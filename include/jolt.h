@@ -387,6 +387,128 @@ int jolt_attend_noalloc(jolt_ctx *ctx, int n_items, const void *const *k_blobs, 
                         const void *v_hdr_host, const int32_t *layers, int n_q, const float *Q,
                         float scale, float *O, jolt_stream stream);
 
+/* ---- Serving a batch of requests from one shared prefix --------------------------------
+ * The prefix is a cell in memory (written by a prefill or by jolt_decompress[_rope]); the
+ * tokens that requests add after it are their tails, kept in pages of a pool that all requests
+ * share.  A step of the batch is: jolt_page_plan (once), then per layer jolt_page_append of the
+ * step's new key and value rows and jolt_prefix_attend of its queries.  All three are
+ * asynchronous, read lengths, tables and maps from device memory only, allocate nothing and may
+ * be captured into a graph and replayed.
+ *
+ * Layout of a pool of pages.  Element (page p, head h, offset o, feature f) lives at
+ *   P + p * stride_page + h * stride_head + o * stride_token + f
+ * (strides in elements, features contiguous, 16-byte aligned bases).  Keys and values are two
+ * pools of one layout, or one allocation with two bases. */
+typedef struct {
+  int32_t dtype;      /* JOLT_F32 or JOLT_BF16 */
+  int32_t n_heads;    /* key-value heads (>= 1) */
+  int32_t page_size;  /* tokens per page: a power of two, 1..1024 */
+  int32_t d;          /* head dimension: 32, 64 or 128 */
+  int32_t n_pages;    /* pages of the pool (>= 1); n_pages * page_size < 2^31 */
+  int32_t reserved;
+  int64_t stride_page, stride_head, stride_token; /* multiples of 8; no two rows overlap */
+} jolt_page_desc;
+
+/* Why jolt_page_plan did not serve a call (bits of info[2]). */
+enum {
+  JOLT_PLAN_NO_PAGES = 1,   /* more new pages needed than n_free (and free_cap) hold */
+  JOLT_PLAN_TABLE_FULL = 2, /* a request needs more than max_pages pages */
+  JOLT_PLAN_NO_TOKENS = 4,  /* the requests add more than n_tok tokens together */
+  JOLT_PLAN_BAD_LENGTH = 8  /* a negative length */
+};
+
+/* Block tables and slot maps of one step, from the requests' lengths (device arrays of int32).
+ *   have, add  [n_req] tokens a request's tail holds and tokens it adds now (0 is fine).
+ *   free_pages [free_cap] a stack of page indices, the top at n_free[0] - 1.  A request takes
+ *              ceil((have + add) / page_size) - ceil(have / page_size) pages; requests take
+ *              them in order, each its own in order, from the top down.
+ *   table      [n_req][max_pages]: page j of request r holds its tokens j * page_size on.  The
+ *              new pages are entered; every other entry keeps its value.
+ *   kv_len     [n_req] have + add.
+ *   q_start    [n_req + 1] running sum of add: request r's new tokens are rows q_start[r] to
+ *              q_start[r + 1] - 1 of the step's packed rows.
+ *   slots, positions [n_tok] of packed row t: its page * page_size + offset, and its index in
+ *              its tail; -1 in both for rows past the last request's.  A table entry or free
+ *              page outside 0..n_pages - 1 gives its rows the slot -1.
+ *   n_free_out [1] what n_free is afterwards (the caller passes it as the next call's n_free,
+ *              and returns pages by writing them on top of the stack).
+ *   info       [4] rows planned, pages taken, 0 or the JOLT_PLAN_* bits of why not, pages that
+ *              the call needs (at most 2^31 - 1).
+ * A call is served as a whole or not at all: where info[2] is not 0 the table is left as it
+ * was, kv_len is have, n_free_out is n_free, q_start is 0 and every slot and position -1, so
+ * that the calls after it write and attend to nothing.
+ * Of the descriptor only page_size and n_pages are used.  n_req <= 4096 (JOLT_E_UNSUPPORTED),
+ * max_pages * page_size < 2^30.
+ * The outputs overlap no input but the table, which is both (kv_len and n_free_out have memory
+ * of their own, since other workgroups still read have and n_free).  Errors: JOLT_E_INVAL. */
+int jolt_page_plan(jolt_ctx *ctx, const jolt_page_desc *pages, int n_req, const int32_t *have,
+                   const int32_t *add, const int32_t *free_pages, int free_cap, const int32_t *n_free,
+                   int32_t *table, int max_pages, int n_tok, int32_t *kv_len, int32_t *q_start,
+                   int32_t *slots, int32_t *positions, int32_t *n_free_out, int32_t *info,
+                   jolt_stream stream);
+
+/* Strided rows of a step: element (row t, head h, feature f) at base + t * stride_token +
+ * h * stride_head + f (strides in elements, multiples of 8, >= 0; 16-byte aligned bases). */
+typedef struct {
+  int64_t stride_token, stride_head;
+} jolt_row_strides;
+
+/* Writes the step's new key and value rows ([n_tok][n_heads][d], of the pool's type) into
+ * their slots; rows with a slot outside 0..n_pages * page_size - 1 are not written, and no slot
+ * may appear twice.  rope (may be NULL): keys are rotated as jolt_rope describes by the
+ * position positions[t] + position_offset (pass the prefix length as the offset), the angle
+ * formed and reduced in fp64, the rotation applied in fp32 and rounded once; values and
+ * unrotated keys are copied bit for bit.  positions may be NULL without rope.
+ * Errors: JOLT_E_INVAL, JOLT_E_UNSUPPORTED (d). */
+int jolt_page_append(jolt_ctx *ctx, const jolt_page_desc *pages, int n_tok, const int32_t *slots,
+                     const int32_t *positions, const jolt_rope *rope, const void *K,
+                     const jolt_row_strides *k_strides, const void *V, const jolt_row_strides *v_strides,
+                     void *K_pages, void *V_pages, jolt_stream stream);
+
+/* The requests of a step as jolt_prefix_attend sees them. */
+typedef struct {
+  int32_t n_req;           /* requests (1..4096) */
+  int32_t n_tok;           /* packed rows of Q and O (>= 1) */
+  int32_t n_q;             /* query heads, a multiple G of the key-value heads; G <= 64 */
+  int32_t max_pages;       /* columns of the table */
+  int32_t max_new;         /* most rows of one request; 0: not known.  It only picks the
+                              kernels: a request with more rows is computed as well, slower */
+  int32_t reserved;
+  int64_t q_stride, o_stride; /* elements between rows of Q and O (multiples of 8, >= n_q * d) */
+} jolt_attend_batch;
+
+/* Attention of a batch of requests over the prefix they share and over each one's own tail.
+ * Row t of request r is token i = t - q_start[r] of its n = q_start[r + 1] - q_start[r] new
+ * ones, the last n of the kv_len[r] tokens of its tail; query head j reads key-value head
+ * j / (n_q / n_heads).  Row t attends to all T tokens of the prefix and to the first
+ * kv_len[r] - n + i + 1 tokens of the tail (none where that is below 1):
+ *   O[t][j] = sum_x softmax_x(scale * Q[t][j] . k_x) v_x,
+ *   lse[t][j] = ln sum_x exp(scale * Q[t][j] . k_x)   (fp32, [n_tok][n_q]; may be NULL).
+ * A row that attends to nothing gets O = 0 and lse = -inf.  What a row does not attend to has
+ * no part in its result, NaN and infinities included.  Rows t of no request are left as they
+ * were.  The keys and values of the prefix are read once for all rows that fit a tile
+ * together, not once per request.
+ *   prefix     layer `layer` of a cell with keys K and values V (one descriptor for both);
+ *              NULL: no prefix.  T < 2^20.
+ *   pages      K_pages, V_pages and table [n_req][max_pages] of the tails; NULL: no tails
+ *              (kv_len and table are then not read).  Lengths are taken as at most
+ *              max_pages * page_size (< 2^30); tokens of a page index outside
+ *              0..n_pages - 1 are not attended to.
+ * Q, O ([n_tok][n_q][d]), prefix and pages are of one type.  bf16: the products are of bf16
+ * values summed in fp32, scores and softmax in fp32, the softmax weights rounded to bf16 for
+ * the value product, O rounded once.  fp32: fp32 throughout.  Results do not depend on the
+ * order of arrival of anything (no atomics): equal calls give equal bits.
+ * O and lse overlap no input.  ws: device, 256-byte aligned, at least
+ * jolt_prefix_attend_workspace_size bytes, not shared by calls that may run at the same time.
+ * Errors: JOLT_E_INVAL, JOLT_E_UNSUPPORTED, JOLT_E_WORKSPACE. */
+int jolt_prefix_attend_workspace_size(const jolt_cell_desc *prefix, const jolt_page_desc *pages,
+                                      const jolt_attend_batch *batch, size_t *bytes);
+int jolt_prefix_attend(jolt_ctx *ctx, const jolt_cell_desc *prefix, const void *K, const void *V, int layer,
+                       const jolt_page_desc *pages, const void *K_pages, const void *V_pages,
+                       const int32_t *table, const jolt_attend_batch *batch, const int32_t *q_start,
+                       const int32_t *kv_len, const void *Q, float scale, void *O, float *lse, void *ws,
+                       size_t ws_bytes, jolt_stream stream);
+
 /* Test hook: copies an intermediate of the most recent jolt_compress on this
  * context for cell `cell` into dst (device memory, dst_bytes): 0 = U_T (T x r_T fp32),
  * 1 = U_d (d x r_d fp32), 2 = X~ (m x T x d fp32 from the stored factors, recomputed by
@@ -451,6 +573,9 @@ enum {
   JOLT_STAGE_SLICE_GRAM,       /* slice-mode Gram of the three-mode diagnostics */
   JOLT_STAGE_ATTEND,           /* decode attention on the factors */
   JOLT_STAGE_TRUNC_GRAM,       /* prefix feature Grams of the token-truncated cell */
+  JOLT_STAGE_PAGE_PLAN,        /* block tables and slot maps of a step */
+  JOLT_STAGE_PAGE_APPEND,      /* new rows into their pages */
+  JOLT_STAGE_PREFIX_ATTEND,    /* attention over a shared prefix and paged tails */
   JOLT_STAGE_COUNT
 };
 int jolt_profile_enable(jolt_ctx *ctx, int on);

@@ -28,6 +28,8 @@ Module map (paper passages in brackets):
   their appendix-A summary (section 3, appendix A).
 * :mod:`oracle.attention` - decode-time softmax attention over the decompressed
   cache (the result a fused attention-on-factors kernel must reproduce; section 8).
+* :mod:`oracle.serving`   - page plans, rotated rows and attention of a batch of requests
+  that share a prefix (loops over requests and tokens).
 
 Parity-unpinned items (no value in the paper can be reproduced on synthetic
 data): the absolute reconstruction errors, the epsilon^2(b) values, the chosen

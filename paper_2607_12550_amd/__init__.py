@@ -23,6 +23,9 @@ __all__ = ["JoltError", "lib", "CellDesc", "SpectrumOpts", "Params", "CellSpectr
            "jolt_eps2_calibrate", "jolt_slice_spectrum_workspace_size", "jolt_slice_spectrum",
            "jolt_mode_summary", "jolt_truncated_spectra_workspace_size", "jolt_truncated_spectra",
            "jolt_attend_workspace_size", "jolt_attend", "jolt_attend_noalloc", "JOLT_ATTEND_SCRATCH_BYTES", "jolt_debug_export", "jolt_debug_set",
+           "PageDesc", "RowStrides", "AttendBatch", "page_desc", "jolt_page_plan", "jolt_page_append",
+           "jolt_prefix_attend_workspace_size", "jolt_prefix_attend", "JOLT_PLAN_NO_PAGES", "JOLT_PLAN_TABLE_FULL",
+           "JOLT_PLAN_NO_TOKENS", "JOLT_PLAN_BAD_LENGTH",
            "jolt_profile_enable", "jolt_profile_reset", "JOLT_E_NONFINITE", "JOLT_E_NOCONV",
            "JOLT_DBG_INVIT_ITERS", "JOLT_DBG_TRD_LANES", "JOLT_DBG_TRD_TWO_STAGE", "JOLT_DBG_BULGE_SPIN", "JOLT_DBG_TRD_GATHER",
            "jolt_profile_read", "STAGES", "cell_desc", "LIB_PATH", "HEADER_PATH"]
@@ -42,6 +45,7 @@ JOLT_DBG_TRD_GATHER = 4
 JOLT_ATTEND_SCRATCH_BYTES = 64 << 20
 JOLT_EXACT, JOLT_FLASH = 0, 1
 JOLT_FACTOR_F32, JOLT_FACTOR_F16 = 0, 1
+JOLT_PLAN_NO_PAGES, JOLT_PLAN_TABLE_FULL, JOLT_PLAN_NO_TOKENS, JOLT_PLAN_BAD_LENGTH = 1, 2, 4, 8
 HEADER_BYTES = 128
 
 
@@ -92,6 +96,21 @@ class Rope(C.Structure):
     _fields_ = [("base", C.c_double), ("position_offset", C.c_int32), ("reserved", C.c_int32)]
 
 
+class PageDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_heads", C.c_int32), ("page_size", C.c_int32), ("d", C.c_int32),
+                ("n_pages", C.c_int32), ("reserved", C.c_int32), ("stride_page", C.c_int64),
+                ("stride_head", C.c_int64), ("stride_token", C.c_int64)]
+
+
+class RowStrides(C.Structure):
+    _fields_ = [("stride_token", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class AttendBatch(C.Structure):
+    _fields_ = [("n_req", C.c_int32), ("n_tok", C.c_int32), ("n_q", C.c_int32), ("max_pages", C.c_int32),
+                ("max_new", C.c_int32), ("reserved", C.c_int32), ("q_stride", C.c_int64), ("o_stride", C.c_int64)]
+
+
 class AllocOpts(C.Structure):
     _fields_ = [("budget_bytes", C.c_double), ("eps2", C.c_double * 4), ("bit_mask", C.c_int32),
                 ("step", C.c_int32), ("floor_rT", C.c_int32), ("floor_rd", C.c_int32),
@@ -136,6 +155,13 @@ _SIGS = {
     "jolt_debug_set": (C.c_int, [_vp, C.c_int, C.c_int64]),
     "jolt_attend_noalloc": (C.c_int, [_vp, C.c_int, _P(_vp), _P(_sz), _P(_vp), _P(_sz), _vp, _vp, _P(_i32),
                                       C.c_int, _vp, C.c_float, _vp, _vp]),
+    "jolt_page_plan": (C.c_int, [_vp, _P(PageDesc), C.c_int, _vp, _vp, _vp, C.c_int, _vp, _vp, C.c_int, C.c_int,
+                                 _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "jolt_page_append": (C.c_int, [_vp, _P(PageDesc), C.c_int, _vp, _vp, _P(Rope), _vp, _P(RowStrides), _vp,
+                                   _P(RowStrides), _vp, _vp, _vp]),
+    "jolt_prefix_attend_workspace_size": (C.c_int, [_P(CellDesc), _P(PageDesc), _P(AttendBatch), _P(_sz)]),
+    "jolt_prefix_attend": (C.c_int, [_vp, _P(CellDesc), _vp, _vp, C.c_int, _P(PageDesc), _vp, _vp, _vp,
+                                     _P(AttendBatch), _vp, _vp, _vp, C.c_float, _vp, _vp, _vp, _sz, _vp]),
     "jolt_profile_enable": (C.c_int, [_vp, C.c_int]),
     "jolt_profile_reset": (C.c_int, [_vp]),
     "jolt_profile_read": (C.c_int, [_vp, C.c_int, _P(_dbl), _P(C.c_int64)]),
@@ -353,7 +379,8 @@ def jolt_eps2_calibrate(ctx, group: int, d: int, seed: int, n_samples: int, ws,
 
 STAGES = ["feature_gram", "token_gram", "tridiag_large", "reserved3", "reserved4", "tridiag_small", "eigvals",
           "eigvecs", "backtransform", "project", "core", "serialize", "reconstruct", "residual",
-          "decode", "sketch", "orth", "slice_gram", "attend", "trunc_gram"]
+          "decode", "sketch", "orth", "slice_gram", "attend", "trunc_gram", "page_plan", "page_append",
+          "prefix_attend"]
 
 
 def jolt_profile_enable(ctx, on: bool = True) -> None:
@@ -435,6 +462,101 @@ def jolt_attend_noalloc(ctx, k_blobs, v_blobs, k_hdr, v_hdr, layers, Q, O, scale
     _check(lib.jolt_attend_noalloc(ctx, n, _ptrs(k_blobs), (_sz * n)(*kb), _ptrs(v_blobs), (_sz * n)(*vb),
                                    kh.ctypes.data, vh.ctypes.data, lay, Q.shape[1], _addr(Q), float(scale),
                                    _addr(O), _stream(stream)))
+
+
+def page_desc(*, dtype, n_heads, page_size, d, n_pages, stride_page, stride_head, stride_token) -> PageDesc:
+    return PageDesc(dtype, n_heads, page_size, d, n_pages, 0, stride_page, stride_head, stride_token)
+
+
+_TORCH_TYPES = {JOLT_F32: torch.float32, JOLT_BF16: torch.bfloat16}
+
+
+def _int32s(name, x, n):
+    """Address of a contiguous int32 tensor of n elements."""
+    if x.dtype != torch.int32 or x.numel() != n or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements")
+    return x.data_ptr()
+
+
+def _rows(name, x, dtype, n_heads, d):
+    """Token and head strides of a [tokens, heads, d] tensor whose features are contiguous."""
+    want = _TORCH_TYPES.get(dtype)
+    if x.dtype != want or x.dim() != 3 or x.shape[1:] != (n_heads, d) or x.stride(2) != 1:
+        raise ValueError(f"{name} must be [tokens, {n_heads}, {d}] of type {want} with contiguous features")
+    # the stride of an axis of one element is never used: it may be anything
+    return RowStrides(x.stride(0) if x.shape[0] > 1 else 0, x.stride(1) if n_heads > 1 else 0)
+
+
+def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, kv_len, q_start, slots, positions,
+                   n_free_out, info, stream=None) -> None:
+    """Block tables and slot maps of a step from the requests' lengths (device int32 tensors):
+    have, add, kv_len [n_req]; q_start [n_req + 1]; table [n_req, max_pages]; slots, positions
+    [n_tok]; n_free, n_free_out [1]; info [4]."""
+    n, n_tok = have.numel(), slots.numel()
+    if table.dim() != 2 or table.shape[0] != n:
+        raise ValueError("table must be [n_req, max_pages]")
+    _check(lib.jolt_page_plan(ctx, C.byref(pages), n, _int32s("have", have, n), _int32s("add", add, n),
+                              _int32s("free_pages", free_pages, free_pages.numel()), free_pages.numel(),
+                              _int32s("n_free", n_free, 1), _int32s("table", table, table.numel()), table.shape[1], n_tok,
+                              _int32s("kv_len", kv_len, n), _int32s("q_start", q_start, n + 1),
+                              _int32s("slots", slots, n_tok), _int32s("positions", positions, n_tok),
+                              _int32s("n_free_out", n_free_out, 1), _int32s("info", info, 4), _stream(stream)))
+
+
+def jolt_page_append(ctx, pages: PageDesc, K, V, slots, K_pages, V_pages, positions=None, rope=None, stream=None) -> None:
+    """Writes the rows K, V [n_tok, n_heads, d] into their slots of the pools; rope: None, or
+    (base, position_offset) to rotate the keys at positions + position_offset."""
+    n = slots.numel()
+    ks, vs = _rows("K", K, pages.dtype, pages.n_heads, pages.d), _rows("V", V, pages.dtype, pages.n_heads, pages.d)
+    if K.shape[0] != n or V.shape[0] != n:
+        raise ValueError("K, V and slots must have the same number of rows")
+    r = None if rope is None else C.byref(Rope(float(rope[0]), int(rope[1]), 0))
+    _check(lib.jolt_page_append(ctx, C.byref(pages), n, _int32s("slots", slots, n),
+                                0 if positions is None else _int32s("positions", positions, n), r, K.data_ptr(),
+                                C.byref(ks), V.data_ptr(), C.byref(vs), _addr(K_pages), _addr(V_pages), _stream(stream)))
+
+
+def jolt_prefix_attend_workspace_size(n_req: int, n_tok: int, n_q: int, prefix=None, pages=None, max_pages: int = 0,
+                                      max_new: int = 0) -> int:
+    d = pages.d if pages is not None else prefix.d if prefix is not None else 0
+    b = AttendBatch(n_req, n_tok, n_q, max_pages, max_new, 0, n_q * d, n_q * d)
+    n = _sz(0)
+    _check(lib.jolt_prefix_attend_workspace_size(None if prefix is None else C.byref(prefix),
+                                                 None if pages is None else C.byref(pages), C.byref(b), C.byref(n)))
+    return n.value
+
+
+def jolt_prefix_attend(ctx, Q, O, q_start, kv_len, scale: float, ws, prefix=None, K_prefix=None, V_prefix=None,
+                       layer: int = 0, pages=None, K_pages=None, V_pages=None, table=None, max_new: int = 0, lse=None,
+                       ws_bytes=None, stream=None) -> None:
+    """Attention of the packed rows Q [n_tok, n_q, d] of a batch over the prefix its requests
+    share (layer `layer` of the cell `prefix`) and each request's own pages; writes O and, if
+    given, lse [n_tok, n_q] fp32.  q_start [n_req + 1], kv_len [n_req], table [n_req, max_pages]
+    are device int32 tensors."""
+    n_req = q_start.numel() - 1
+    desc = pages if pages is not None else prefix
+    if desc is None:
+        raise ValueError("a prefix or pages are needed")
+    if Q.dim() != 3 or Q.shape != O.shape or Q.shape[2] != desc.d:
+        raise ValueError(f"Q and O must be [n_tok, n_q, {desc.d}]")
+    n_tok, n_q, d = Q.shape
+    want = _TORCH_TYPES.get(desc.dtype)
+    for name, x in (("Q", Q), ("O", O)):
+        if x.dtype != want or x.stride(2) != 1 or (n_q > 1 and x.stride(1) != d):
+            raise ValueError(f"{name} must be of type {want} with contiguous rows")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_tok, n_q) or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous fp32 tensor [n_tok, n_q]")
+    max_pages, tab, lens = 0, 0, 0
+    if pages is not None:
+        if table.dim() != 2 or table.shape[0] != n_req:
+            raise ValueError("table must be [n_req, max_pages]")
+        max_pages, tab, lens = table.shape[1], _int32s("table", table, table.numel()), _int32s("kv_len", kv_len, n_req)
+    b = AttendBatch(n_req, n_tok, n_q, max_pages, max_new, 0, *(x.stride(0) if n_tok > 1 else n_q * d for x in (Q, O)))
+    wsb = ws_bytes if ws_bytes is not None else (ws.numel() * ws.element_size())
+    _check(lib.jolt_prefix_attend(ctx, None if prefix is None else C.byref(prefix), _addr(K_prefix), _addr(V_prefix), layer,
+                                  None if pages is None else C.byref(pages), _addr(K_pages), _addr(V_pages), tab, C.byref(b),
+                                  _int32s("q_start", q_start, n_req + 1), lens, Q.data_ptr(), float(scale), O.data_ptr(),
+                                  _addr(lse), _addr(ws), wsb, _stream(stream)))
 
 
 def jolt_debug_export(ctx, what: int, cell: int, dst, stream=None) -> None:

@@ -231,6 +231,50 @@ constexpr int ATTN_SCRATCH_DEVICES = 64;
 // the calling thread must have `device` current
 hipError_t attend_scratch_address(int device, void **ptr);
 
+// ----------------------------------------------------------------- serving from a shared prefix
+constexpr int SERVE_REQ_MAX = 4096;   // requests of a call
+constexpr int SERVE_PAGE_MAX = 1024;  // tokens of a page
+constexpr int SERVE_REP_MAX = 64;     // query heads per key-value head
+struct PagePlanArgs {
+  const int32_t *have, *add, *free_pages, *n_free;
+  int32_t *table, *kv_len, *q_start, *slots, *positions, *n_free_out, *info;
+  int32_t n_req, free_cap, max_pages, n_tok, n_pages, page_shift;
+};
+hipError_t launch_page_plan(const PagePlanArgs &a, hipStream_t st);
+
+struct PageAppendArgs {
+  const int32_t *slots, *positions;
+  const void *K, *V;
+  void *Kp, *Vp;
+  int64_t k_tok, k_head, v_tok, v_head;        // strides of the rows, in elements
+  int64_t s_page, s_head, s_tok;               // strides of the pools, in elements
+  int32_t n_tok, n_heads, page_shift, n_slots; // n_slots = n_pages * page_size
+  int32_t rope, offset;
+  double turns[64];                            // base^(-2 j / d) / (2 pi): turns per position
+};
+hipError_t launch_page_append(const PageAppendArgs &a, int d, int dtype, hipStream_t st);
+
+// Where the rows of keys and values lie: token x of a run sits at
+// page[x >> shift] * s_page + (x & mask) * s_tok + head * s_head; the prefix is one page.
+struct PrefixSource {
+  const void *K, *V;
+  int64_t s_page, s_head, s_tok;
+  int32_t shift, n_pages;
+};
+struct PrefixAttendArgs {
+  PrefixSource prefix, tail;
+  const int32_t *table, *q_start, *kv_len;     // table = null: no tails
+  const void *Q;
+  void *O;
+  float *lse;
+  int64_t q_stride, o_stride;
+  int32_t n_req, n_tok, n_q, heads, group;     // group = n_q / heads
+  int32_t T, max_pages, max_new;               // T = 0: no prefix
+  float scale;
+};
+size_t prefix_attend_workspace(const PrefixAttendArgs &a, int d);
+hipError_t launch_prefix_attend(const PrefixAttendArgs &a, int d, int dtype, void *ws, hipStream_t st);
+
 // ----------------------------------------------------------------- eigensolver
 struct EigBatch {
   float *A;              // [n_mat][n][n] row-major; lower triangle read, overwritten with
