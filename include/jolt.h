@@ -471,8 +471,8 @@ typedef struct {
   int32_t n_tok;           /* packed rows of Q and O (>= 1) */
   int32_t n_q;             /* query heads, a multiple G of the key-value heads; G <= 64 */
   int32_t max_pages;       /* columns of the table */
-  int32_t max_new;         /* most rows of one request; 0: not known.  It only picks the
-                              kernels: a request with more rows is computed as well, slower */
+  int32_t max_new;         /* most rows of one request; 0: not known (n_tok is then taken).  It
+                              picks the kernels; a request with more rows counts as having none */
   int32_t reserved;
   int64_t q_stride, o_stride; /* elements between rows of Q and O (multiples of 8, >= n_q * d) */
 } jolt_attend_batch;

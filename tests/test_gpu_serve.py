@@ -265,11 +265,15 @@ def test_prefix_attend(dtype, case):
     b.check(b.run(), want)                  # the bound on new rows not given
 
 
-def test_prefix_attend_bound_on_new_rows_is_a_hint():
-    """A request with more rows than max_new says is computed all the same."""
+def test_prefix_attend_bound_on_new_rows():
+    """A request with more rows than max_new says counts as having none: its rows stay as they were."""
     b = Batch("bf16", 100, [3, 0, 50], [1, 60, 9], 2, 2, 64, 16)
-    want = b.want()
-    for m in (1, 2, 8, 9, 59, 10 ** 6):
+    for m in (1, 2, 8, 9, 59, 60, 61, 10 ** 6):
+        want = b.want()
+        for r, n in enumerate((1, 60, 9)):
+            if n > m:
+                for w in want:
+                    w[b.q_start[r]:b.q_start[r + 1]] = np.nan
         b.check(b.run(max_new=m), want)
 
 
