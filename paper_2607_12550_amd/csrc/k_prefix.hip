@@ -6,12 +6,13 @@
 // run keeps the running maximum m (in units of log2) and sum l of its softmax and the sum of
 // exp2(s - m) v, and the last kernel joins the runs of a row.
 //
-//  * k_few:  at most 16 NQ rows.  Reading the keys and values bounds it, so the four waves of a
+//  * few:  at most 16 NQ rows.  Reading the keys and values bounds it, so the four waves of a
 //    workgroup take different tokens of the run, keys go from memory straight into the matrix
 //    operand, and only the values pass through LDS (a region of the wave's own) to be transposed.
-//  * k_many: 64 NQ rows a workgroup, which share the tiles of keys and values in LDS: the
+//  * many: 64 NQ rows a workgroup, which share the tiles of keys and values in LDS: the
 //    prefix is read once per row tile instead of once per request, and the matrix cores bound it.
 //  * k_join: the runs of a row.
+// k_runs holds few and many, for the prefix and for the tails, in one launch.
 //
 // Products are formed transposed, S^T = K Q^T and O^T = V^T P^T: the matrix instruction then
 // leaves the scores of 4 neighbouring tokens of one query in a lane, which are the weights that
@@ -37,12 +38,10 @@ struct Geo {
   static constexpr bool BF = sizeof(T) == 2;
   static constexpr int SUB = BF ? 2 : 1, TPW = 16 * SUB;   // groups of 16 tokens, tokens, of a wave's step
   static constexpr int TILE = BF ? 64 : 32;                // tokens of a shared tile
-  // Pieces of an LDS row are permuted in pairs by row, so that the 16 rows that one transposed
-  // read touches (32 bytes each) fall in distinct banks.
-  static JOLT_DEV int swz(int row, int piece) {
-    constexpr int RL = RB >= 256 ? 1 : 256 / RB, PM = (RB >= 256 ? 256 : RB) / 32 - 1;
-    return piece ^ (((row / RL) & PM) << 1);
-  }
+  // Bytes of a row in LDS, padded so that what one instruction reads falls in distinct banks and
+  // every address is a lane's base plus a constant: 16 rows x 16 bytes of keys; of values 8 rows x
+  // 32 bytes by the transposed reads (bf16), rows 4 apart x 64 bytes (fp32).
+  static constexpr int KP = RB + 16, VP = RB + (BF ? 32 : 16);
 };
 
 template <class T>
@@ -101,41 +100,41 @@ JOLT_DEV int request_of(const PrefixAttendArgs &a, int t, int lane) {
   return t >= x.q0 && t < x.q0 + x.n ? lo : -1;
 }
 
-// Runs of the requests that k_few serves: at most FEW_ITEMS / heads runs besides one a request,
+// Runs of the requests that few() serves: at most FEW_ITEMS / heads runs besides one a request,
 // of equal length (a multiple of the tokens a workgroup takes a step), in the requests' order.
 // Every workgroup forms the sums for itself; the result is in LDS.
-constexpr int FEW_ITEMS = 1024, RUN_STEP = 128;
-struct Item { int r, first, last; };   // request, tokens first .. last - 1
+constexpr int FEW_ITEMS = 512, RUN_STEP = 128;
 JOLT_DEV int few_run(int64_t total, int heads) {
   const int64_t c = (total * heads + FEW_ITEMS - 1) / FEW_ITEMS;
   return (int)((max(c, (int64_t)RUN_STEP) + RUN_STEP - 1) / RUN_STEP * RUN_STEP);
 }
 
-JOLT_DEV int64_t wave_scan(int64_t v, int lane) {   // inclusive
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int64_t u = __shfl_up(v, m, 64);
-    if (lane >= m) v += u;
-  }
-  return v;
-}
-
-struct FindLds { int64_t sum[WAVES]; int cnt[WAVES]; int r, idx; };
-// Item `want` of the call (kind 0: runs of k_few's requests, kind 1: row tiles of k_many's), or
-// r = -1 past the last; item_first (workgroups that write it): [n_req + 1] first run of each.
+struct FindLds {
+  int64_t sum[WAVES];
+  int cnt[WAVES];
+  int r, idx, run;
+  Req x;
+};
+// Item `want` of the call (kind 0: runs of few's requests, kind 1: row tiles of many's): its
+// request and its place there, or r = -1 past the last; item_first (if given): [n_req + 1] first
+// item of each request.
 template <int KIND>
-JOLT_DEV void find_item(const PrefixAttendArgs &a, int want, int limit, int rows_tile, int32_t *item_first, int &run, FindLds &sm) {
+JOLT_DEV void find_item(const PrefixAttendArgs &a, int want, int limit, int rows_tile, int32_t *item_first, FindLds &sm) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (a.n_req + NT - 1) / NT, r0 = min(tid * per, a.n_req), r1 = min(r0 + per, a.n_req);
-  run = 0;
+  Req x0{0, 0, 0};
+  if (r0 < r1) x0 = request(a, r0);
+  auto at = [&](int r) { return r == r0 ? x0 : request(a, r); };
+  int run = RUN_STEP;
   if constexpr (KIND == 0) {
     int64_t total = 0;
     for (int r = r0; r < r1; ++r) {
-      const Req x = request(a, r);
+      const Req x = at(r);
       if (x.n > 0 && x.n * a.group <= limit) total += x.len;
     }
-    const int64_t w = wave_scan(total, lane);
-    if (lane == 63) sm.sum[wave] = w;
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) total += __shfl_xor(total, m, 64);
+    if (lane == 0) sm.sum[wave] = total;
     __syncthreads();
     total = 0;
     for (int i = 0; i < WAVES; ++i) total += sm.sum[i];
@@ -147,7 +146,7 @@ JOLT_DEV void find_item(const PrefixAttendArgs &a, int want, int limit, int rows
     else return rows > limit ? (rows + rows_tile - 1) / rows_tile : 0;
   };
   int mine = 0;
-  for (int r = r0; r < r1; ++r) mine += count(request(a, r));
+  for (int r = r0; r < r1; ++r) mine += count(at(r));
   int incl = mine;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
@@ -161,9 +160,15 @@ JOLT_DEV void find_item(const PrefixAttendArgs &a, int want, int limit, int rows
   for (int w = 0; w < wave; ++w) before += sm.cnt[w];
   if (item_first || (want >= before && want < before + mine)) {
     for (int r = r0; r < r1; ++r) {
-      const int c = count(request(a, r));
+      const Req x = at(r);
+      const int c = count(x);
       if (item_first) item_first[r] = before;
-      if (want >= before && want < before + c) { sm.r = r; sm.idx = want - before; }
+      if (want >= before && want < before + c) {
+        sm.r = r;
+        sm.idx = want - before;
+        sm.run = run;
+        sm.x = x;
+      }
       before += c;
     }
     if (item_first && r1 == a.n_req && r0 < r1) item_first[a.n_req] = before;
@@ -238,11 +243,11 @@ struct Rows {
       l[x] += sum;
     }
   }
-  // o += V^T P^T for 16 SUBS tokens whose values stand in LDS rows row0 ..; the weights are
+  // o += V^T P^T for 16 SUBS tokens whose values stand in LDS; the weights are
   // rounded to bf16 for the bf16 product (values are bf16 already): half a step each, which
   // averages out over the tokens, for half of the matrix work of two terms.
   template <int SUBS>
-  JOLT_DEV void values(const f4_t (&p)[SUBS][NQ], const uint8_t *v, int row0, int n16, int g) {
+  JOLT_DEV void values(const f4_t (&p)[SUBS][NQ], const uint8_t *v, int n16, int g) {
     if constexpr (G::BF) {
 #pragma unroll
       for (int u = 0; u < SUBS; u += 2) {
@@ -253,12 +258,11 @@ struct Rows {
                                  pack_bf16(p[u + 1][x][0], p[u + 1][x][1]), pack_bf16(p[u + 1][x][2], p[u + 1][x][3])};
           __builtin_memcpy(&w[x], d, 16);
         }
-        const int ra = row0 + 16 * u + 4 * g + (n16 >> 2), rb = ra + 16;
+        const uint8_t *base = v + (4 * g + (n16 >> 2)) * G::VP + 8 * (n16 & 3);
 #pragma unroll
         for (int f = 0; f < G::FT; ++f) {
-          const int piece = 2 * f + ((n16 >> 1) & 1), low = 8 * (n16 & 1);
-          auto *pa = v + ra * G::RB + G::swz(ra, piece) * 16 + low;
-          auto *pb = v + rb * G::RB + G::swz(rb, piece) * 16 + low;
+          auto *pa = base + 16 * u * G::VP + 32 * f;
+          auto *pb = pa + 16 * G::VP;
           const s4_t xa = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t *)pa);
           const s4_t xb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t *)pb);
           const auto xv = __builtin_shufflevector(xa, xb, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -273,10 +277,10 @@ struct Rows {
       for (int u = 0; u < SUBS; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int r = row0 + 16 * u + 4 * g + i;
+          const uint8_t *base = v + 4 * g * G::VP + 4 * n16;
 #pragma unroll
           for (int f = 0; f < G::FT; ++f) {
-            const float va = *reinterpret_cast<const float *>(v + r * G::RB + G::swz(r, 4 * f + (n16 >> 2)) * 16 + 4 * (n16 & 3));
+            const float va = *reinterpret_cast<const float *>(base + (16 * u + i) * G::VP + 64 * f);
 #pragma unroll
             for (int x = 0; x < NQ; ++x) o[f][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(va, p[u][x][i], o[f][x], 0, 0, 0);
           }
@@ -295,7 +299,7 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int byte = (e0 + i) * (int)sizeof(T);
-          const T raw = *reinterpret_cast<const T *>(v + k * G::RB + G::swz(k, byte >> 4) * 16 + (byte & 15));
+          const T raw = *reinterpret_cast<const T *>(v + k * G::VP + byte);
           float val;
           if constexpr (G::BF) val = bf16_to_f32(raw); else val = raw;
 #pragma unroll
@@ -353,7 +357,6 @@ struct Parts {
 
 // ------------------------------------------------------------------------------- few rows
 struct FewArgs {
-  PrefixAttendArgs a;
   Parts out;
   int32_t *item_first;      // tails: first run of each request
   int32_t rows;             // rows kept per run and head: row rho of head h at (item * heads + h) * rows + rho
@@ -361,32 +364,32 @@ struct FewArgs {
   int32_t run;              // prefix: tokens of a run
 };
 
+template <int D, class T, int NQ>
+struct FewLds {
+  static constexpr int VB = Geo<D, T>::TPW * Geo<D, T>::VP, OB = 16 * NQ * D * 4;   // a wave's values, its output
+  static constexpr int WB = VB > OB ? VB : OB;
+  uint8_t w[WAVES][WB];
+  float m[WAVES][16 * NQ], l[WAVES][16 * NQ];
+  FindLds f;
+};
+
 template <int D, class T, int NQ, bool TAIL>
-__global__ void __launch_bounds__(NT) k_few(const FewArgs p) {
+JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds<D, T, NQ> &sm) {
   using G = Geo<D, T>;
-  constexpr int VB = G::TPW * G::RB;                     // a wave's values
-  constexpr int OB = 16 * NQ * D * 4;                    // a wave's output
-  constexpr int WB = VB > OB ? VB : OB;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[WAVES * WB];
-  __shared__ float sm_m[WAVES][16 * NQ], sm_l[WAVES][16 * NQ];
-  __shared__ FindLds fl;
-  const PrefixAttendArgs &a = p.a;
   const PrefixSource &src = TAIL ? a.tail : a.prefix;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % a.heads, item = blockIdx.x / a.heads;
-  int t0, n, first, end;
+  const int h = block % a.heads, item = block / a.heads;
+  int t0, n, first, end, len = 0;
   const int32_t *pages = nullptr;
   if constexpr (TAIL) {
-    int run;
-    find_item<0>(a, item, p.limit, 0, blockIdx.x == 0 ? p.item_first : nullptr, run, fl);
-    const int r = fl.r;
-    if (r < 0) return;
-    const Req x = request(a, r);
-    t0 = x.q0;
-    n = x.n;
-    first = fl.idx * run;
-    end = min(x.len, first + run);
-    pages = a.table + (int64_t)r * a.max_pages;
+    find_item<0>(a, item, p.limit, 0, block == 0 ? p.item_first : nullptr, sm.f);
+    if (sm.f.r < 0) return;
+    t0 = sm.f.x.q0;
+    n = sm.f.x.n;
+    len = sm.f.x.len;
+    first = sm.f.idx * sm.f.run;
+    end = min(len, first + sm.f.run);
+    pages = a.table + (int64_t)sm.f.r * a.max_pages;
   } else {
     t0 = 0;
     n = a.n_tok;
@@ -399,16 +402,15 @@ __global__ void __launch_bounds__(NT) k_few(const FewArgs p) {
   R.clear();
   int seen_all = 0x7fffffff;         // tokens that every row sees
   if constexpr (TAIL) {
-    const Req x = request(a, fl.r);
 #pragma unroll
     for (int c = 0; c < NQ; ++c) {
       const int rho = 16 * c + n16;
-      R.seen[c] = rho < n_rows ? max(0, x.len - x.n + rho / a.group + 1) : 0x7fffffff;
+      R.seen[c] = rho < n_rows ? max(0, len - n + rho / a.group + 1) : 0x7fffffff;
     }
-    seen_all = max(0, x.len - x.n + 1);
+    seen_all = max(0, len - n + 1);
   }
   const float c = a.scale * LOG2E;
-  uint8_t *vl = lds + wave * WB;
+  uint8_t *vl = sm.w[wave];
   const uint8_t *Kb = static_cast<const uint8_t *>(src.K), *Vb = static_cast<const uint8_t *>(src.V);
   ju4 kr[G::SUB][G::KS], vr[G::SUB][G::KS];
   RowAt at[G::SUB];
@@ -489,8 +491,7 @@ __global__ void __launch_bounds__(NT) k_few(const FewArgs p) {
       for (int u = 0; u < G::SUB; ++u)
 #pragma unroll
         for (int k = 0; k < G::KS; ++k) {
-          const int row = 16 * u + n16;
-          *reinterpret_cast<ju4 *>(vl + row * G::RB + G::swz(row, 4 * k + g) * 16) = vr[u][k];
+          *reinterpret_cast<ju4 *>(vl + (16 * u + n16) * G::VP + 64 * k + 16 * g) = vr[u][k];
         }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
@@ -511,32 +512,32 @@ __global__ void __launch_bounds__(NT) k_few(const FewArgs p) {
       }
     }
     if (more) load(Vb, vr);
-    R.values(s, vl, 0, n16, g);
+    R.values(s, vl, n16, g);
   }
   // the waves' results join in LDS
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     const float l = over_groups_sum(R.l[q]);
-    if (g == 0) { sm_m[wave][16 * q + n16] = R.m[q]; sm_l[wave][16 * q + n16] = l; }
+    if (g == 0) { sm.m[wave][16 * q + n16] = R.m[q]; sm.l[wave][16 * q + n16] = l; }
 #pragma unroll
     for (int f = 0; f < G::FT; ++f)
       *reinterpret_cast<f4_t *>(vl + ((16 * q + n16) * D + 16 * f + 4 * g) * 4) = R.o[f][q];
   }
   __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * p.rows;     // (item * heads + h) * rows
+  const int64_t base = (int64_t)block * p.rows;          // (item * heads + h) * rows
   for (int i = tid; i < n_rows * (D / 4); i += NT) {
     const int row = i / (D / 4), e = (i % (D / 4)) * 4;
-    float M = sm_m[0][row];
+    float M = sm.m[0][row];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm_m[w][row]);
+    for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm.m[w][row]);
     f4_t o = {0, 0, 0, 0};
     float l = 0.f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_m[w][row] - M);
-      if (sm_m[w][row] != -INFINITY || sm_l[w][row] != 0.f) {
-        l = fmaf(sm_l[w][row], al, l);
-        o += *reinterpret_cast<const f4_t *>(lds + w * WB + (row * D + e) * 4) * al;
+      const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm.m[w][row] - M);
+      if (sm.m[w][row] != -INFINITY || sm.l[w][row] != 0.f) {
+        l = fmaf(sm.l[w][row], al, l);
+        o += *reinterpret_cast<const f4_t *>(sm.w[w] + (row * D + e) * 4) * al;
       }
     }
     *reinterpret_cast<f4_t *>(p.out.o + (base + row) * D + e) = o;
@@ -546,43 +547,42 @@ __global__ void __launch_bounds__(NT) k_few(const FewArgs p) {
 
 // ------------------------------------------------------------------------------- many rows
 struct ManyArgs {
-  PrefixAttendArgs a;
   Parts out;                // [split][packed row][query head]
   int32_t splits, tiles;    // prefix: row tiles; tails: most row tiles of the call
   int32_t limit;            // tails: requests of more rows per head than this
 };
 
+template <int D, class T>
+struct ManyLds {
+  uint8_t k[2][Geo<D, T>::TILE * Geo<D, T>::KP], v[2][Geo<D, T>::TILE * Geo<D, T>::VP];   // [buffer]
+  int there[2][Geo<D, T>::TILE];
+  int flag[2];
+  FindLds f;
+};
+
 template <int D, class T, int NQ, bool TAIL>
-__global__ void __launch_bounds__(NT) k_many(const ManyArgs p) {
+JOLT_DEV void many(const PrefixAttendArgs &a, const ManyArgs &p, int block, ManyLds<D, T> &sm) {
   using G = Geo<D, T>;
   constexpr int RT = 64 * NQ, SUBS = G::TILE / 16;
   constexpr int PASS = NT / G::CH, LOADS = G::TILE / PASS;   // rows of a load, loads of a tile
   static_assert(G::TILE % PASS == 0, "a tile is whole loads");
-  constexpr int TB = G::TILE * G::RB;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TB];
-  __shared__ int there[2][G::TILE];
-  __shared__ int flag[2];
-  __shared__ FindLds fl;
-  const PrefixAttendArgs &a = p.a;
   const PrefixSource &src = TAIL ? a.tail : a.prefix;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % a.heads, rest = blockIdx.x / a.heads;
+  const int h = block % a.heads, rest = block / a.heads;
   const int tile = rest % p.tiles, split = rest / p.tiles;
-  int t0, n, len, rho0, seen_all = 0x7fffffff;
+  int t0, n, len, tail_len = 0, rho0, seen_all = 0x7fffffff;
   const int32_t *pages = nullptr;
   if constexpr (TAIL) {
-    int run;
-    find_item<1>(a, tile, p.limit, RT, nullptr, run, fl);
-    const int r = fl.r;
-    if (r < 0) return;
-    const Req x = request(a, r);
-    t0 = x.q0;
-    n = x.n;
-    rho0 = fl.idx * RT;
+    find_item<1>(a, tile, p.limit, RT, nullptr, sm.f);
+    if (sm.f.r < 0) return;
+    t0 = sm.f.x.q0;
+    n = sm.f.x.n;
+    tail_len = sm.f.x.len;
+    rho0 = sm.f.idx * RT;
     // the tile's last row sees most, its first least
-    len = max(0, x.len - x.n + min(x.n, (rho0 + RT - 1) / a.group + 1));
-    seen_all = max(0, x.len - x.n + rho0 / a.group + 1);
-    pages = a.table + (int64_t)r * a.max_pages;
+    len = max(0, tail_len - n + min(n, (rho0 + RT - 1) / a.group + 1));
+    seen_all = max(0, tail_len - n + rho0 / a.group + 1);
+    pages = a.table + (int64_t)sm.f.r * a.max_pages;
   } else {
     t0 = 0;
     n = a.n_tok;
@@ -597,11 +597,10 @@ __global__ void __launch_bounds__(NT) k_many(const ManyArgs p) {
   R.load(a, h, t0, rho_w, n_rows, n16, g);
   R.clear();
   if constexpr (TAIL) {
-    const Req x = request(a, fl.r);
 #pragma unroll
     for (int c = 0; c < NQ; ++c) {
       const int rho = rho_w + 16 * c + n16;
-      R.seen[c] = rho < n_rows ? max(0, x.len - x.n + rho / a.group + 1) : 0x7fffffff;
+      R.seen[c] = rho < n_rows ? max(0, tail_len - n + rho / a.group + 1) : 0x7fffffff;
     }
   }
   const float c = a.scale * LOG2E;
@@ -627,16 +626,16 @@ __global__ void __launch_bounds__(NT) k_many(const ManyArgs p) {
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int row = i * PASS + lrow, at = row * G::RB + G::swz(row, piece) * 16;
+      const int row = i * PASS + lrow;
       if (!ok[i]) vr[i] = ju4{0, 0, 0, 0};
-      *reinterpret_cast<ju4 *>(&lds[b][0][at]) = kr[i];
-      *reinterpret_cast<ju4 *>(&lds[b][1][at]) = vr[i];
-      if (piece == 0) there[b][row] = ok[i];
+      *reinterpret_cast<ju4 *>(&sm.k[b][row * G::KP + piece * 16]) = kr[i];
+      *reinterpret_cast<ju4 *>(&sm.v[b][row * G::VP + piece * 16]) = vr[i];
+      if (piece == 0) sm.there[b][row] = ok[i];
       if constexpr (TAIL) bad |= nonfinite<T>(vr[i]);
     }
-    if (TAIL && x + G::TILE > seen_all && bad) flag[b] = 1;
+    if (TAIL && x + G::TILE > seen_all && bad) sm.flag[b] = 1;
   };
-  if (TAIL && tid < 2) flag[tid] = 0;
+  if (TAIL && tid < 2) sm.flag[tid] = 0;
   if (first < end) {
     ask_pages(first);
     load(first);
@@ -651,17 +650,16 @@ __global__ void __launch_bounds__(NT) k_many(const ManyArgs p) {
       load(x + G::TILE);
       ask_pages(x + 2 * G::TILE);
     }
-    const uint8_t *kl = lds[b][0];
-    uint8_t *vl = lds[b][1];
+    const uint8_t *kl = sm.k[b] + n16 * G::KP + 16 * g;
+    uint8_t *vl = sm.v[b];
     f4_t s[SUBS][NQ];
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
 #pragma unroll
       for (int q = 0; q < NQ; ++q) s[u][q] = f4_t{0, 0, 0, 0};
-      const int row = 16 * u + n16;
 #pragma unroll
       for (int k = 0; k < G::KS; ++k) {
-        const ju4 ka = *reinterpret_cast<const ju4 *>(kl + row * G::RB + G::swz(row, 4 * k + g) * 16);
+        const ju4 ka = *reinterpret_cast<const ju4 *>(kl + 16 * u * G::KP + 64 * k);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) s[u][q] = product_step<T>(ka, R.q[q][k], s[u][q]);
       }
@@ -672,26 +670,26 @@ __global__ void __launch_bounds__(NT) k_many(const ManyArgs p) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int k = 16 * u + 4 * g + i;
-          const bool in = there[b][k] != 0;
+          const bool in = sm.there[b][k] != 0;
 #pragma unroll
           for (int q = 0; q < NQ; ++q)
             if (!in || (TAIL && x + k >= R.seen[q])) s[u][q][i] = -INFINITY;
         }
     }
     R.softmax(s, c);
-    if (TAIL && flag[b]) {          // the same for all threads: written before the last barrier
+    if (TAIL && sm.flag[b]) {          // the same for all threads: written before the last barrier
       R.template add_nonfinite<G::TILE>(vl, x, n16, g);
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int row = i * PASS + lrow;
-        ju4 *at = reinterpret_cast<ju4 *>(vl + row * G::RB + G::swz(row, piece) * 16);
+        ju4 *at = reinterpret_cast<ju4 *>(vl + row * G::VP + piece * 16);
         *at = finite_or_zero<T>(*at);
       }
-      if (tid == 0) flag[b] = 0;
+      if (tid == 0) sm.flag[b] = 0;
       __syncthreads();
     }
-    R.values(s, vl, 0, n16, g);
+    R.values(s, vl, n16, g);
     if (more) put(b ^ 1, x + G::TILE);
     __syncthreads();
   }
@@ -709,59 +707,120 @@ __global__ void __launch_bounds__(NT) k_many(const ManyArgs p) {
   }
 }
 
+// ------------------------------------------------------------------------------- all runs
+// One launch for the runs of the prefix and of the tails: the first fill the matrix cores while
+// the others wait for memory, and no part waits for the last workgroup of another.
+enum { ROLE_NONE = 0, ROLE_FEW1, ROLE_FEW2, ROLE_MANY1, ROLE_MANY2 };
+struct RunArgs {
+  PrefixAttendArgs a;
+  FewArgs pre_few, few;
+  ManyArgs pre_many, many;
+  int32_t pre_role, few_role, many_role;
+  int32_t n_pre, n_many, n_few;        // workgroups, in this order
+};
+
+template <int D, class T>
+union RunLds {
+  FewLds<D, T, 1> f1;
+  FewLds<D, T, 2> f2;
+  ManyLds<D, T> m;
+};
+
+template <int D, class T>
+__global__ void __launch_bounds__(NT, 2) k_runs(const RunArgs p) {
+  __shared__ __attribute__((aligned(16))) RunLds<D, T> sm;
+  int b = blockIdx.x;
+  if (b < p.n_pre) {
+    if (p.pre_role == ROLE_FEW1) few<D, T, 1, false>(p.a, p.pre_few, b, sm.f1);
+    else if (p.pre_role == ROLE_FEW2) few<D, T, 2, false>(p.a, p.pre_few, b, sm.f2);
+    else if (p.pre_role == ROLE_MANY1) many<D, T, 1, false>(p.a, p.pre_many, b, sm.m);
+    else many<D, T, 2, false>(p.a, p.pre_many, b, sm.m);
+    return;
+  }
+  b -= p.n_pre;
+  if (b < p.n_many) {
+    if (p.many_role == ROLE_MANY1) many<D, T, 1, true>(p.a, p.many, b, sm.m);
+    else many<D, T, 2, true>(p.a, p.many, b, sm.m);
+    return;
+  }
+  b -= p.n_many;
+  if (p.few_role == ROLE_FEW1) few<D, T, 1, true>(p.a, p.few, b, sm.f1);
+  else few<D, T, 2, true>(p.a, p.few, b, sm.f2);
+}
+
 // ------------------------------------------------------------------------------- join
 struct JoinArgs {
   PrefixAttendArgs a;
   Parts prefix, few, many;
   const int32_t *item_first;
-  int32_t n_prefix, prefix_few;   // runs of the prefix; laid out as k_few's
+  int32_t n_prefix, prefix_few;   // runs of the prefix; laid out as few's
   int32_t few_rows, prefix_rows, limit;
-  int32_t n_many;                 // splits of the tails of k_many's requests
+  int32_t n_many;                 // splits of the tails of many's requests
 };
 
-// One wave per row and query head.
+// One wave per row and query head.  A lane takes one run's maximum and sum, so that the weights of
+// 64 runs are known at once and the rows that they weigh are read without waiting for each other.
 template <int D, class T>
 __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
   constexpr int E = D >= 128 ? 2 : 1;
+  typedef float vec __attribute__((ext_vector_type(E)));
   const PrefixAttendArgs &a = p.a;
   const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
-  if (id >= (int64_t)a.n_tok * a.n_q) return;
-  const int t = (int)(id / a.n_q), j = (int)(id % a.n_q), h = j / a.group, jj = j % a.group;
+  const int id = (int)(blockIdx.x * WAVES + (threadIdx.x >> 6));
+  if (id >= a.n_tok * a.n_q) return;
+  const int t = id / a.n_q, j = id - t * a.n_q, h = j / a.group, jj = j - h * a.group;
   const int r = request_of(a, t, lane);
   if (r < 0) return;
   const Req x = request(a, r);
-  float M = -INFINITY, l = 0.f, o[E] = {};
-  const bool has = lane * E < D;
-  auto add = [&](const Parts &s, int64_t row) {
-    const float2 ml = s.ml[row];
-    if (ml.x == -INFINITY && ml.y == 0.f) return;   // an empty run
-    const float mn = fmaxf(M, ml.x);
-    const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
-    const float be = __builtin_amdgcn_exp2f(ml.x - mn);
-    M = mn;
-    l = fmaf(l, al, ml.y * be);
+  const int i0 = lane * E < D ? lane * E : 0;
+  float M = -INFINITY, l = 0.f;
+  vec o = 0.f;
+  // runs 0 .. n - 1 of a part, run i's row at base + i * step
+  auto add = [&](const Parts &s, int n, int64_t base, int64_t step) {
+    for (int i = 0; i < n; i += 64) {
+      const int c = min(64, n - i);
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < c) ml = s.ml[base + (i + lane) * step];
+      float mn = ml.x;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], al, has ? s.o[row * D + lane * E + e] * be : 0.f);
+      for (int k = 32; k >= 1; k >>= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
+      mn = fmaxf(mn, M);
+      // an empty run weighs nothing, whatever its row holds
+      const float w = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - mn);
+      const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
+      M = mn;
+      l = fmaf(l, al, wave_sum(ml.y * w));
+      o *= al;
+      const float *row = s.o + (base + i * step) * D + i0;
+      for (int k = 0; k < c; k += 8) {
+        vec v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const vec *>(row + min(k + u, c - 1) * step * D);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {      // lanes past c weigh nothing
+          const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k + u));
+          if (wk != 0.f) o += v[u] * wk;
+        }
+      }
+    }
   };
-  for (int s = 0; s < p.n_prefix; ++s)
-    add(p.prefix, p.prefix_few ? ((int64_t)s * a.heads + h) * p.prefix_rows + t * a.group + jj : ((int64_t)s * a.n_tok + t) * a.n_q + j);
+  if (p.prefix_few) add(p.prefix, p.n_prefix, (int64_t)h * p.prefix_rows + t * a.group + jj, (int64_t)a.heads * p.prefix_rows);
+  else add(p.prefix, p.n_prefix, id, (int64_t)a.n_tok * a.n_q);
   if (a.table) {
     if (x.n * a.group <= p.limit) {
-      const int i1 = p.item_first[r + 1];
-      for (int i = p.item_first[r]; i < i1; ++i) add(p.few, ((int64_t)i * a.heads + h) * p.few_rows + (t - x.q0) * a.group + jj);
+      const int f0 = p.item_first[r];
+      add(p.few, p.item_first[r + 1] - f0, ((int64_t)f0 * a.heads + h) * p.few_rows + (t - x.q0) * a.group + jj, (int64_t)a.heads * p.few_rows);
     } else {
-      for (int s = 0; s < p.n_many; ++s) add(p.many, ((int64_t)s * a.n_tok + t) * a.n_q + j);
+      add(p.many, p.n_many, id, (int64_t)a.n_tok * a.n_q);
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (has) {
+  if (lane * E < D) {
     T *O = static_cast<T *>(a.O) + (int64_t)t * a.o_stride + (int64_t)j * D + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float v = o[e] * inv;
-      if constexpr (sizeof(T) == 2) O[e] = f32_to_bf16(v); else O[e] = v;
-    }
+    o *= inv;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<vec *>(O) = o;
+    else if constexpr (E == 2) *reinterpret_cast<uint32_t *>(O) = pack_bf16(o[0], o[1]);
+    else *O = f32_to_bf16(o[0]);
   }
   if (a.lse && lane == 0) a.lse[id] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
 }
@@ -779,6 +838,22 @@ constexpr int BLOCKS = 512;        // workgroups that fill the chip: two a CU
 
 int64_t ceil_div(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
+// Splits of a prefix of T tokens for `blocks` row tiles: the cheapest by a model in units of a
+// 64-token tile of a workgroup that has its CU to itself (about 1.2 us).  Two workgroups of a
+// CU take 1.5 times as long as one; a workgroup starts and ends in about 3 tiles; and every
+// split's output (`out` floats) is written and read once more, at about 4 MB a us.
+int splits(int64_t blocks, int64_t T, int64_t out) {
+  double best = 0;
+  int pick = 1;
+  for (int s = 1; s <= 64 && (s == 1 || T >= 128 * s); ++s) {
+    const int64_t n = blocks * s, rem = n % BLOCKS;
+    const double rounds = 1.5 * (n / BLOCKS) + (rem == 0 ? 0 : rem <= BLOCKS / 2 ? 1 : 1.5);
+    const double cost = rounds * ((double)ceil_div(ceil_div(T, s), 64) + 3) + s * (double)out * 8 / (4e6 * 1.2);
+    if (s == 1 || cost < best) { best = cost; pick = s; }
+  }
+  return pick;
+}
+
 Cut cut(const PrefixAttendArgs &a, int d, bool tails) {
   Cut c;
   const int64_t rows = (int64_t)a.n_tok * a.group;     // rows of a key-value head
@@ -791,8 +866,7 @@ Cut cut(const PrefixAttendArgs &a, int d, bool tails) {
       c.n_prefix = (int)ceil_div(a.T, c.prefix_run);
     } else {
       c.prefix_tiles = (int)ceil_div(rows, 64 * c.prefix_nq);
-      const int64_t want = BLOCKS / ((int64_t)a.heads * c.prefix_tiles);
-      c.n_prefix = (int)std::max<int64_t>(1, std::min<int64_t>(want, ceil_div(a.T, 256)));
+      c.n_prefix = splits((int64_t)a.heads * c.prefix_tiles, a.T, (int64_t)a.n_tok * a.n_q * d);
     }
   }
   if (tails) {
@@ -833,29 +907,28 @@ hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t
   auto parts = [&](size_t o, size_t m) { return Parts{reinterpret_cast<float *>(ws + o), reinterpret_cast<float2 *>(ws + m)}; };
   const Parts pp = parts(c.off_po, c.off_pm), pf = parts(c.off_fo, c.off_fm), pm = parts(c.off_mo, c.off_mm);
   int32_t *items = reinterpret_cast<int32_t *>(ws + c.off_items);
+  RunArgs p{};
+  p.a = a;
   if (a.T > 0 && c.prefix_few) {
-    const FewArgs p{a, pp, nullptr, a.n_tok * a.group, 0, c.prefix_run};
-    const int grid = c.n_prefix * a.heads;
-    if (c.prefix_nq == 1) k_few<D, T, 1, false><<<grid, NT, 0, st>>>(p);
-    else k_few<D, T, 2, false><<<grid, NT, 0, st>>>(p);
+    p.pre_few = FewArgs{pp, nullptr, a.n_tok * a.group, 0, c.prefix_run};
+    p.pre_role = c.prefix_nq == 1 ? ROLE_FEW1 : ROLE_FEW2;
+    p.n_pre = c.n_prefix * a.heads;
   } else if (a.T > 0) {
-    const ManyArgs p{a, pp, c.n_prefix, c.prefix_tiles, 0};
-    const int grid = c.n_prefix * c.prefix_tiles * a.heads;
-    if (c.prefix_nq == 1) k_many<D, T, 1, false><<<grid, NT, 0, st>>>(p);
-    else k_many<D, T, 2, false><<<grid, NT, 0, st>>>(p);
-  }
-  if (c.tails_few) {
-    const FewArgs p{a, pf, items, c.few_rows, c.limit, 0};
-    const int grid = c.few_items * a.heads;
-    if (c.few_nq == 1) k_few<D, T, 1, true><<<grid, NT, 0, st>>>(p);
-    else k_few<D, T, 2, true><<<grid, NT, 0, st>>>(p);
+    p.pre_many = ManyArgs{pp, c.n_prefix, c.prefix_tiles, 0};
+    p.pre_role = c.prefix_nq == 1 ? ROLE_MANY1 : ROLE_MANY2;
+    p.n_pre = c.n_prefix * c.prefix_tiles * a.heads;
   }
   if (c.tails_many) {
-    const ManyArgs p{a, pm, c.n_many, c.many_tiles, c.limit};
-    const int grid = c.n_many * c.many_tiles * a.heads;
-    if (c.many_nq == 1) k_many<D, T, 1, true><<<grid, NT, 0, st>>>(p);
-    else k_many<D, T, 2, true><<<grid, NT, 0, st>>>(p);
+    p.many = ManyArgs{pm, c.n_many, c.many_tiles, c.limit};
+    p.many_role = c.many_nq == 1 ? ROLE_MANY1 : ROLE_MANY2;
+    p.n_many = c.n_many * c.many_tiles * a.heads;
   }
+  if (c.tails_few) {
+    p.few = FewArgs{pf, items, c.few_rows, c.limit, 0};
+    p.few_role = c.few_nq == 1 ? ROLE_FEW1 : ROLE_FEW2;
+    p.n_few = c.few_items * a.heads;
+  }
+  k_runs<D, T><<<p.n_pre + p.n_many + p.n_few, NT, 0, st>>>(p);
   const JoinArgs j{a, pp, pf, pm, items, c.n_prefix, c.prefix_few, c.few_rows, a.n_tok * a.group, c.limit, c.n_many};
   k_join<D, T><<<(int)ceil_div((int64_t)a.n_tok * a.n_q, WAVES), NT, 0, st>>>(j);
   return hipGetLastError();
