@@ -84,48 +84,37 @@ JOLT_DEV Req request(const PrefixAttendArgs &a, int r) {
   return x;
 }
 
-// The request of packed row t, or -1: the last one that starts at or before t, found by the
-// whole wave (64 candidates a step, two steps at most).
-JOLT_DEV int request_of(const PrefixAttendArgs &a, int t, int lane) {
-  int lo = 0, step = a.n_req > 64 ? 64 : 1;
-  for (;; step = 1) {
-    const int r = lo + lane * step;
-    const bool in = r < a.n_req && a.q_start[r] <= t;
-    const int c = __popcll(__ballot(in));
-    if (c == 0) return -1;
-    lo += (c - 1) * step;
-    if (step == 1) break;
-  }
-  const Req x = request(a, lo);
-  return t >= x.q0 && t < x.q0 + x.n ? lo : -1;
-}
-
-// Runs of the requests that few() serves: at most FEW_ITEMS / heads runs besides one a request,
-// of equal length (a multiple of the tokens a workgroup takes a step), in the requests' order.
-// Every workgroup forms the sums for itself; the result is in LDS.
-constexpr int FEW_ITEMS = 512, RUN_STEP = 128;
+// Runs of the requests that few() serves: of equal length (a multiple of a wave's step), about
+// FEW_WAVES runs of a head over all heads besides one a request, in the requests' order.  Every
+// workgroup forms the sums for itself, from one read of the lengths.
+constexpr int FEW_WAVES = 2048, RUN_MIN = 128, RUN_STEP = 32;
 JOLT_DEV int few_run(int64_t total, int heads) {
-  const int64_t c = (total * heads + FEW_ITEMS - 1) / FEW_ITEMS;
-  return (int)((max(c, (int64_t)RUN_STEP) + RUN_STEP - 1) / RUN_STEP * RUN_STEP);
+  const int64_t c = (total * heads + FEW_WAVES - 1) / FEW_WAVES;
+  return (int)((max(c, (int64_t)RUN_MIN) + RUN_STEP - 1) / RUN_STEP * RUN_STEP);
 }
 
+// What the join needs to know of a packed row: its place in its request, whose runs are items
+// first .. first + count - 1 of few() (kind 0) or the splits of many() (kind 1); kind -1: the row
+// is of no request.
+struct RowEntry { int first, count, place, kind; };
+
+struct Found { int r, idx, run; Req x; };
+template <int W>
 struct FindLds {
   int64_t sum[WAVES];
   int cnt[WAVES];
-  int r, idx, run;
-  Req x;
+  Found at[W];
 };
-// Item `want` of the call (kind 0: runs of few's requests, kind 1: row tiles of many's): its
-// request and its place there, or r = -1 past the last; item_first (if given): [n_req + 1] first
-// item of each request.
-template <int KIND>
-JOLT_DEV void find_item(const PrefixAttendArgs &a, int want, int limit, int rows_tile, int32_t *item_first, FindLds &sm) {
+// Items want[0 .. W - 1] of the call (kind 0: runs of few's requests, kind 1: row tiles of
+// many's): their requests and places there, or r = -1 past the last.
+template <int KIND, int W>
+JOLT_DEV void find_items(const PrefixAttendArgs &a, const int (&want)[W], int limit, int rows_tile, RowEntry *entries, FindLds<W> &sm) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (a.n_req + NT - 1) / NT, r0 = min(tid * per, a.n_req), r1 = min(r0 + per, a.n_req);
   Req x0{0, 0, 0};
   if (r0 < r1) x0 = request(a, r0);
   auto at = [&](int r) { return r == r0 ? x0 : request(a, r); };
-  int run = RUN_STEP;
+  int run = RUN_MIN;
   if constexpr (KIND == 0) {
     int64_t total = 0;
     for (int r = r0; r < r1; ++r) {
@@ -154,24 +143,50 @@ JOLT_DEV void find_item(const PrefixAttendArgs &a, int want, int limit, int rows
     if (lane >= m) incl += u;
   }
   if (lane == 63) sm.cnt[wave] = incl;
-  if (tid == 0) sm.r = -1;
+  if (tid < W) sm.at[tid].r = -1;
   __syncthreads();
   int before = incl - mine;
   for (int w = 0; w < wave; ++w) before += sm.cnt[w];
-  if (item_first || (want >= before && want < before + mine)) {
+  bool here = false;
+#pragma unroll
+  for (int w = 0; w < W; ++w) here |= want[w] >= before && want[w] < before + mine;
+  if (here) {
+    int b = before;
     for (int r = r0; r < r1; ++r) {
       const Req x = at(r);
       const int c = count(x);
-      if (item_first) item_first[r] = before;
-      if (want >= before && want < before + c) {
-        sm.r = r;
-        sm.idx = want - before;
-        sm.run = run;
-        sm.x = x;
-      }
-      before += c;
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+        if (want[w] >= b && want[w] < b + c) sm.at[w] = Found{r, want[w] - b, run, x};
+      b += c;
     }
-    if (item_first && r1 == a.n_req && r0 < r1) item_first[a.n_req] = before;
+  }
+  if (entries) {
+    // rows outside q_start[0] .. q_start[n_req], then every request's: a lane its own where they
+    // are few, the wave together where they are many
+    const int s0 = min(max(a.q_start[0], 0), a.n_tok), s1 = min(max(a.q_start[a.n_req], 0), a.n_tok);
+    for (int t = tid; t < s0; t += NT) entries[t].kind = -1;
+    for (int t = s1 + tid; t < a.n_tok; t += NT) entries[t].kind = -1;
+    for (int i = 0; i < per; ++i) {
+      const int r = r0 + i;
+      Req x{0, 0, 0};
+      int n_all = 0, c = 0;
+      if (r < r1) {
+        x = at(r);
+        n_all = min(max(a.q_start[r + 1], x.q0), a.n_tok) - x.q0;   // with those past the bound
+        c = count(x);
+      }
+      RowEntry e{before, c, 0, n_all > x.n ? -1 : x.n * a.group <= limit ? 0 : 1};
+      before += c;
+      if (n_all <= 8)
+        for (int k = 0; k < n_all; ++k) { e.place = k; entries[x.q0 + k] = e; }
+      for (uint64_t m = __ballot(n_all > 8); m; m &= m - 1) {
+        const int src = __builtin_ctzll(m);
+        const int q0 = __shfl(x.q0, src, 64), nn = __shfl(n_all, src, 64);
+        RowEntry f{__shfl(e.first, src, 64), __shfl(e.count, src, 64), 0, __shfl(e.kind, src, 64)};
+        for (int k = lane; k < nn; k += 64) { f.place = k; entries[q0 + k] = f; }
+      }
+    }
   }
   __syncthreads();
 }
@@ -356,9 +371,11 @@ struct Parts {
 };
 
 // ------------------------------------------------------------------------------- few rows
+// A workgroup takes one run of the prefix, its waves every fourth step of it, and joins their
+// results; of the tails, which are short, every wave takes a run of its own.
 struct FewArgs {
   Parts out;
-  int32_t *item_first;      // tails: first run of each request
+  RowEntry *entries;        // tails: [n_tok]
   int32_t rows;             // rows kept per run and head: row rho of head h at (item * heads + h) * rows + rho
   int32_t limit;            // tails: requests of at most this many rows per head
   int32_t run;              // prefix: tokens of a run
@@ -370,7 +387,7 @@ struct FewLds {
   static constexpr int WB = VB > OB ? VB : OB;
   uint8_t w[WAVES][WB];
   float m[WAVES][16 * NQ], l[WAVES][16 * NQ];
-  FindLds f;
+  FindLds<WAVES> f;
 };
 
 template <int D, class T, int NQ, bool TAIL>
@@ -378,18 +395,24 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
   using G = Geo<D, T>;
   const PrefixSource &src = TAIL ? a.tail : a.prefix;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, g = lane >> 4;
-  const int h = block % a.heads, item = block / a.heads;
+  const int id = TAIL ? block * WAVES + wave : block;      // item * heads + h
+  const int h = id % a.heads, item = id / a.heads;
+  constexpr int STRIDE = TAIL ? G::TPW : WAVES * G::TPW;   // tokens from a wave's step to its next
   int t0, n, first, end, len = 0;
   const int32_t *pages = nullptr;
   if constexpr (TAIL) {
-    find_item<0>(a, item, p.limit, 0, block == 0 ? p.item_first : nullptr, sm.f);
-    if (sm.f.r < 0) return;
-    t0 = sm.f.x.q0;
-    n = sm.f.x.n;
-    len = sm.f.x.len;
-    first = sm.f.idx * sm.f.run;
-    end = min(len, first + sm.f.run);
-    pages = a.table + (int64_t)sm.f.r * a.max_pages;
+    int want[WAVES];
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) want[w] = (block * WAVES + w) / a.heads;
+    find_items<0, WAVES>(a, want, p.limit, 0, block == 0 ? p.entries : nullptr, sm.f);
+    const Found f = sm.f.at[wave];
+    if (f.r < 0) return;
+    t0 = f.x.q0;
+    n = f.x.n;
+    len = f.x.len;
+    first = f.idx * f.run;
+    end = min(len, first + f.run);
+    pages = a.table + (int64_t)f.r * a.max_pages;
   } else {
     t0 = 0;
     n = a.n_tok;
@@ -415,7 +438,7 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
   ju4 kr[G::SUB][G::KS], vr[G::SUB][G::KS];
   RowAt at[G::SUB];
   int pg[G::SUB];
-  const int x0 = first + wave * G::TPW;
+  const int x0 = first + (TAIL ? 0 : wave * G::TPW);
   auto ask_pages = [&](int x) {
 #pragma unroll
     for (int u = 0; u < G::SUB; ++u) pg[u] = page_of(src, pages, x + 16 * u + n16, end);
@@ -435,9 +458,9 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
     place(x0);
     load(Kb, kr);
     load(Vb, vr);
-    ask_pages(x0 + WAVES * G::TPW);
+    ask_pages(x0 + STRIDE);
   }
-  for (int x = x0; x < end; x += WAVES * G::TPW) {
+  for (int x = x0; x < end; x += STRIDE) {
     f4_t s[G::SUB][NQ];
 #pragma unroll
     for (int u = 0; u < G::SUB; ++u)
@@ -458,12 +481,12 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
     bool mine[G::SUB];
 #pragma unroll
     for (int u = 0; u < G::SUB; ++u) mine[u] = at[u].ok;
-    const int xn = x + WAVES * G::TPW;
+    const int xn = x + STRIDE;
     const bool more = xn < end;
     if (more) {
       place(xn);
       load(Kb, kr);
-      ask_pages(xn + WAVES * G::TPW);
+      ask_pages(xn + STRIDE);
     }
     if (!whole || partly) {
 #pragma unroll
@@ -514,6 +537,20 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
     if (more) load(Vb, vr);
     R.values(s, vl, n16, g);
   }
+  const int64_t base = (int64_t)id * p.rows;
+  if constexpr (TAIL) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const float l = over_groups_sum(R.l[q]);
+      const int rho = 16 * q + n16;
+      if (rho < n_rows) {
+#pragma unroll
+        for (int f = 0; f < G::FT; ++f) *reinterpret_cast<f4_t *>(p.out.o + (base + rho) * D + 16 * f + 4 * g) = R.o[f][q];
+        if (g == 0) p.out.ml[base + rho] = make_float2(R.m[q], l);
+      }
+    }
+    return;
+  }
   // the waves' results join in LDS
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
@@ -524,7 +561,6 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
       *reinterpret_cast<f4_t *>(vl + ((16 * q + n16) * D + 16 * f + 4 * g) * 4) = R.o[f][q];
   }
   __syncthreads();
-  const int64_t base = (int64_t)block * p.rows;          // (item * heads + h) * rows
   for (int i = tid; i < n_rows * (D / 4); i += NT) {
     const int row = i / (D / 4), e = (i % (D / 4)) * 4;
     float M = sm.m[0][row];
@@ -557,7 +593,7 @@ struct ManyLds {
   uint8_t k[2][Geo<D, T>::TILE * Geo<D, T>::KP], v[2][Geo<D, T>::TILE * Geo<D, T>::VP];   // [buffer]
   int there[2][Geo<D, T>::TILE];
   int flag[2];
-  FindLds f;
+  FindLds<1> f;
 };
 
 template <int D, class T, int NQ, bool TAIL>
@@ -573,16 +609,18 @@ JOLT_DEV void many(const PrefixAttendArgs &a, const ManyArgs &p, int block, Many
   int t0, n, len, tail_len = 0, rho0, seen_all = 0x7fffffff;
   const int32_t *pages = nullptr;
   if constexpr (TAIL) {
-    find_item<1>(a, tile, p.limit, RT, nullptr, sm.f);
-    if (sm.f.r < 0) return;
-    t0 = sm.f.x.q0;
-    n = sm.f.x.n;
-    tail_len = sm.f.x.len;
-    rho0 = sm.f.idx * RT;
+    const int want[1] = {tile};
+    find_items<1, 1>(a, want, p.limit, RT, nullptr, sm.f);
+    const Found f = sm.f.at[0];
+    if (f.r < 0) return;
+    t0 = f.x.q0;
+    n = f.x.n;
+    tail_len = f.x.len;
+    rho0 = f.idx * RT;
     // the tile's last row sees most, its first least
     len = max(0, tail_len - n + min(n, (rho0 + RT - 1) / a.group + 1));
     seen_all = max(0, tail_len - n + rho0 / a.group + 1);
-    pages = a.table + (int64_t)sm.f.r * a.max_pages;
+    pages = a.table + (int64_t)f.r * a.max_pages;
   } else {
     t0 = 0;
     n = a.n_tok;
@@ -752,9 +790,9 @@ __global__ void __launch_bounds__(NT, 2) k_runs(const RunArgs p) {
 struct JoinArgs {
   PrefixAttendArgs a;
   Parts prefix, few, many;
-  const int32_t *item_first;
+  const RowEntry *entries;
   int32_t n_prefix, prefix_few;   // runs of the prefix; laid out as few's
-  int32_t few_rows, prefix_rows, limit;
+  int32_t few_rows, prefix_rows, few_items;
   int32_t n_many;                 // splits of the tails of many's requests
 };
 
@@ -769,9 +807,12 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
   const int id = (int)(blockIdx.x * WAVES + (threadIdx.x >> 6));
   if (id >= a.n_tok * a.n_q) return;
   const int t = id / a.n_q, j = id - t * a.n_q, h = j / a.group, jj = j - h * a.group;
-  const int r = request_of(a, t, lane);
-  if (r < 0) return;
-  const Req x = request(a, r);
+  // starts that do not rise leave entries unwritten or written twice: nothing is read by an entry
+  // that is out of bounds
+  RowEntry e = p.entries[t];
+  if (e.kind != 0 && e.kind != 1) return;
+  e.first = min(max(e.first, 0), p.few_items);
+  e.count = min(max(e.count, 0), p.few_items - e.first);
   const int i0 = lane * E < D ? lane * E : 0;
   float M = -INFINITY, l = 0.f;
   vec o = 0.f;
@@ -806,13 +847,11 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
   };
   if (p.prefix_few) add(p.prefix, p.n_prefix, (int64_t)h * p.prefix_rows + t * a.group + jj, (int64_t)a.heads * p.prefix_rows);
   else add(p.prefix, p.n_prefix, id, (int64_t)a.n_tok * a.n_q);
-  if (a.table) {
-    if (x.n * a.group <= p.limit) {
-      const int f0 = p.item_first[r];
-      add(p.few, p.item_first[r + 1] - f0, ((int64_t)f0 * a.heads + h) * p.few_rows + (t - x.q0) * a.group + jj, (int64_t)a.heads * p.few_rows);
-    } else {
-      add(p.many, p.n_many, id, (int64_t)a.n_tok * a.n_q);
-    }
+  if (e.kind == 0) {
+    const int rho = min(max(e.place, 0) * a.group + jj, p.few_rows - 1);
+    add(p.few, e.count, ((int64_t)e.first * a.heads + h) * p.few_rows + rho, (int64_t)a.heads * p.few_rows);
+  } else {
+    add(p.many, p.n_many, id, (int64_t)a.n_tok * a.n_q);
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (lane * E < D) {
@@ -828,54 +867,64 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
 // ------------------------------------------------------------------------------- launches
 // How a call is cut, from its sizes alone (the workspace depends on it too).
 struct Cut {
-  bool prefix_few = false, tails_few = false, tails_many = false;
+  bool prefix_few = false, tails_many = false;
   int prefix_nq = 1, prefix_run = 0, n_prefix = 0, prefix_tiles = 0;   // of k_few / k_many
   int few_nq = 1, few_items = 0, few_rows = 0, limit = 0;
   int many_nq = 1, many_tiles = 0, n_many = 0;
-  size_t off_po, off_pm, off_fo, off_fm, off_mo, off_mm, off_items, total;
+  size_t off_po, off_pm, off_fo, off_fm, off_mo, off_mm, off_entries, total;
 };
 constexpr int BLOCKS = 512;        // workgroups that fill the chip: two a CU
 
 int64_t ceil_div(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
-// Splits of a prefix of T tokens for `blocks` row tiles: the cheapest by a model in units of a
-// 64-token tile of a workgroup that has its CU to itself (about 1.2 us).  Two workgroups of a
-// CU take 1.5 times as long as one; a workgroup starts and ends in about 3 tiles; and every
-// split's output (`out` floats) is written and read once more, at about 4 MB a us.
-int splits(int64_t blocks, int64_t T, int64_t out) {
+// Row tiles and splits of the prefix for many(): the cheapest by a model in us.  A workgroup that
+// has its CU to itself takes about `tile` us a tile of keys and values (the matrix work, and a
+// part that waits for memory and LDS) and 4 us to start and end; two on a CU take 1.5 times as
+// long as one; every split's output is written and read once more, at about 4 MB a us.
+void cut_prefix(Cut &c, const PrefixAttendArgs &a, int d, bool bf16) {
+  const int64_t rows = (int64_t)a.n_tok * a.group, tokens = bf16 ? 64 : 32;
+  const double out = (double)a.n_tok * a.n_q * d * 8 / 4e6;
   double best = 0;
-  int pick = 1;
-  for (int s = 1; s <= 64 && (s == 1 || T >= 128 * s); ++s) {
-    const int64_t n = blocks * s, rem = n % BLOCKS;
-    const double rounds = 1.5 * (n / BLOCKS) + (rem == 0 ? 0 : rem <= BLOCKS / 2 ? 1 : 1.5);
-    const double cost = rounds * ((double)ceil_div(ceil_div(T, s), 64) + 3) + s * (double)out * 8 / (4e6 * 1.2);
-    if (s == 1 || cost < best) { best = cost; pick = s; }
+  c.n_prefix = 0;
+  for (int nq = 1; nq <= 2; ++nq) {
+    const int64_t tiles = ceil_div(rows, 64 * nq);
+    const double tile = 0.3 + (bf16 ? 0.9 : 3.4) * d / 128 * nq / 2;
+    for (int s = 1; s <= 64 && (s == 1 || a.T >= tokens * s); ++s) {
+      const int64_t n = a.heads * tiles * s, rem = n % BLOCKS;
+      const double rounds = 1.5 * (n / BLOCKS) + (rem == 0 ? 0 : rem <= BLOCKS / 2 ? 1 : 1.5);
+      const double cost = rounds * (tile * ceil_div(ceil_div(a.T, s), tokens) + 4) + s * out;
+      if (c.n_prefix == 0 || cost < best) {
+        best = cost;
+        c.n_prefix = s;
+        c.prefix_nq = nq;
+        c.prefix_tiles = (int)tiles;
+      }
+    }
   }
-  return pick;
 }
 
-Cut cut(const PrefixAttendArgs &a, int d, bool tails) {
+Cut cut(const PrefixAttendArgs &a, int d, bool bf16) {
   Cut c;
   const int64_t rows = (int64_t)a.n_tok * a.group;     // rows of a key-value head
   if (a.T > 0) {
     c.prefix_few = rows <= 32;
-    c.prefix_nq = c.prefix_few ? (rows <= 16 ? 1 : 2) : (rows <= 64 ? 1 : 2);
     if (c.prefix_few) {
-      const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(ceil_div(a.T, RUN_STEP), BLOCKS / a.heads));
-      c.prefix_run = (int)(ceil_div(ceil_div(a.T, runs), RUN_STEP) * RUN_STEP);
+      c.prefix_nq = rows <= 16 ? 1 : 2;
+      const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(ceil_div(a.T, RUN_MIN), BLOCKS / a.heads));
+      c.prefix_run = (int)(ceil_div(ceil_div(a.T, runs), RUN_MIN) * RUN_MIN);
       c.n_prefix = (int)ceil_div(a.T, c.prefix_run);
     } else {
-      c.prefix_tiles = (int)ceil_div(rows, 64 * c.prefix_nq);
-      c.n_prefix = splits((int64_t)a.heads * c.prefix_tiles, a.T, (int64_t)a.n_tok * a.n_q * d);
+      cut_prefix(c, a, d, bf16);
     }
   }
-  if (tails) {
+  // without tails every request is one of few rows and no runs
+  c.limit = 0x7fffffff;
+  if (a.max_pages > 0) {
     const int64_t most = (int64_t)a.max_new * a.group; // rows of a request
     c.few_nq = most <= 16 ? 1 : 2;
     c.limit = 16 * c.few_nq;
-    c.tails_few = true;
     c.few_rows = (int)std::min<int64_t>(most, c.limit);
-    c.few_items = FEW_ITEMS / a.heads + a.n_req;
+    c.few_items = FEW_WAVES / a.heads + a.n_req;
     c.tails_many = most > c.limit;
     if (c.tails_many) {
       c.many_nq = most <= 64 ? 1 : 2;
@@ -897,7 +946,7 @@ Cut cut(const PrefixAttendArgs &a, int d, bool tails) {
   c.off_po = take(np * d * 4); c.off_pm = take(np * 8);
   c.off_fo = take(nf * d * 4); c.off_fm = take(nf * 8);
   c.off_mo = take(nm * d * 4); c.off_mm = take(nm * 8);
-  c.off_items = take(((size_t)a.n_req + 1) * 4);
+  c.off_entries = take((size_t)a.n_tok * sizeof(RowEntry));
   c.total = off;
   return c;
 }
@@ -906,7 +955,7 @@ template <int D, class T>
 hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t st) {
   auto parts = [&](size_t o, size_t m) { return Parts{reinterpret_cast<float *>(ws + o), reinterpret_cast<float2 *>(ws + m)}; };
   const Parts pp = parts(c.off_po, c.off_pm), pf = parts(c.off_fo, c.off_fm), pm = parts(c.off_mo, c.off_mm);
-  int32_t *items = reinterpret_cast<int32_t *>(ws + c.off_items);
+  RowEntry *entries = reinterpret_cast<RowEntry *>(ws + c.off_entries);
   RunArgs p{};
   p.a = a;
   if (a.T > 0 && c.prefix_few) {
@@ -923,23 +972,22 @@ hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t
     p.many_role = c.many_nq == 1 ? ROLE_MANY1 : ROLE_MANY2;
     p.n_many = c.n_many * c.many_tiles * a.heads;
   }
-  if (c.tails_few) {
-    p.few = FewArgs{pf, items, c.few_rows, c.limit, 0};
-    p.few_role = c.few_nq == 1 ? ROLE_FEW1 : ROLE_FEW2;
-    p.n_few = c.few_items * a.heads;
-  }
+  // the first workgroup of these schedules, also where there are no tails
+  p.few = FewArgs{pf, entries, c.few_rows, c.limit, 0};
+  p.few_role = c.few_nq == 1 ? ROLE_FEW1 : ROLE_FEW2;
+  p.n_few = (int)std::max<int64_t>(1, ceil_div((int64_t)c.few_items * a.heads, WAVES));
   k_runs<D, T><<<p.n_pre + p.n_many + p.n_few, NT, 0, st>>>(p);
-  const JoinArgs j{a, pp, pf, pm, items, c.n_prefix, c.prefix_few, c.few_rows, a.n_tok * a.group, c.limit, c.n_many};
+  const JoinArgs j{a, pp, pf, pm, entries, c.n_prefix, c.prefix_few, c.few_rows, a.n_tok * a.group, c.few_items, c.n_many};
   k_join<D, T><<<(int)ceil_div((int64_t)a.n_tok * a.n_q, WAVES), NT, 0, st>>>(j);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t prefix_attend_workspace(const PrefixAttendArgs &a, int d) { return cut(a, d, a.max_pages > 0).total; }
+size_t prefix_attend_workspace(const PrefixAttendArgs &a, int d, int dtype) { return cut(a, d, dtype == JOLT_BF16).total; }
 
 hipError_t launch_prefix_attend(const PrefixAttendArgs &a, int d, int dtype, void *ws, hipStream_t st) {
-  const Cut c = cut(a, d, a.max_pages > 0);
+  const Cut c = cut(a, d, dtype == JOLT_BF16);
   uint8_t *w = static_cast<uint8_t *>(ws);
   if (dtype == JOLT_BF16)
     return d == 32 ? run<32, bf16_t>(a, c, w, st) : d == 64 ? run<64, bf16_t>(a, c, w, st) : run<128, bf16_t>(a, c, w, st);

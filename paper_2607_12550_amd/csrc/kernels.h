@@ -272,7 +272,7 @@ struct PrefixAttendArgs {
   int32_t T, max_pages, max_new;               // T = 0: no prefix
   float scale;
 };
-size_t prefix_attend_workspace(const PrefixAttendArgs &a, int d);
+size_t prefix_attend_workspace(const PrefixAttendArgs &a, int d, int dtype);
 hipError_t launch_prefix_attend(const PrefixAttendArgs &a, int d, int dtype, void *ws, hipStream_t st);
 
 // ----------------------------------------------------------------- eigensolver

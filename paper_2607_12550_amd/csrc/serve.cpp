@@ -181,7 +181,7 @@ extern "C" int jolt_prefix_attend_workspace_size(const jolt_cell_desc *prefix, c
   int rc = resolve_prefix_attend(prefix, pages, batch, &a, &d, &dtype);
   if (rc) return rc;
   if (!bytes) return jolt_fail(JOLT_E_INVAL, "bytes is null");
-  *bytes = prefix_attend_workspace(a, d);
+  *bytes = prefix_attend_workspace(a, d, dtype);
   return JOLT_OK;
 }
 
@@ -205,7 +205,7 @@ extern "C" int jolt_prefix_attend(jolt_ctx *ctx, const jolt_cell_desc *prefix, c
     return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: Q, O, keys and values must be 16-byte aligned");
   if (misaligned(ws, 256)) return jolt_fail(JOLT_E_INVAL, "workspace must be 256-byte aligned");
   if (!(scale > 0.f) || !std::isfinite(scale)) return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: scale must be > 0");
-  const size_t need = prefix_attend_workspace(a, d);
+  const size_t need = prefix_attend_workspace(a, d, dtype);
   if (ws_bytes < need) return jolt_fail(JOLT_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   if (!ctx) return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: ctx is null");
   DeviceGuard dg;
