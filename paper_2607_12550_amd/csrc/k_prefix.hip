@@ -87,7 +87,7 @@ JOLT_DEV Req request(const PrefixAttendArgs &a, int r) {
 // Runs of the requests that few() serves: of equal length (a multiple of a wave's step), about
 // FEW_WAVES runs of a head over all heads besides one a request, in the requests' order.  Every
 // workgroup forms the sums for itself, from one read of the lengths.
-constexpr int FEW_WAVES = 2048, RUN_MIN = 128, RUN_STEP = 32;
+constexpr int FEW_WAVES = 2048, RUN_MIN = 32, RUN_STEP = 32, RUN_PREFIX = 128;
 JOLT_DEV int few_run(int64_t total, int heads) {
   const int64_t c = (total * heads + FEW_WAVES - 1) / FEW_WAVES;
   return (int)((max(c, (int64_t)RUN_MIN) + RUN_STEP - 1) / RUN_STEP * RUN_STEP);
@@ -797,25 +797,20 @@ struct JoinArgs {
 };
 
 // One wave per row and query head.  A lane takes one run's maximum and sum, so that the weights of
-// 64 runs are known at once and the rows that they weigh are read without waiting for each other.
+// 64 runs are known at once and the rows that they weigh are read without waiting for each other:
+// D / 4 lanes a row, 256 / D runs a load, four loads at a time.
 template <int D, class T>
 __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
-  constexpr int E = D >= 128 ? 2 : 1;
-  typedef float vec __attribute__((ext_vector_type(E)));
+  constexpr int LR = D / 4, RL = 64 / LR;      // lanes of a row, rows of a load
   const PrefixAttendArgs &a = p.a;
   const int lane = threadIdx.x & 63;
   const int id = (int)(blockIdx.x * WAVES + (threadIdx.x >> 6));
   if (id >= a.n_tok * a.n_q) return;
   const int t = id / a.n_q, j = id - t * a.n_q, h = j / a.group, jj = j - h * a.group;
-  // starts that do not rise leave entries unwritten or written twice: nothing is read by an entry
-  // that is out of bounds
+  const int sub = lane / LR, col = (lane % LR) * 4;
   RowEntry e = p.entries[t];
-  if (e.kind != 0 && e.kind != 1) return;
-  e.first = min(max(e.first, 0), p.few_items);
-  e.count = min(max(e.count, 0), p.few_items - e.first);
-  const int i0 = lane * E < D ? lane * E : 0;
   float M = -INFINITY, l = 0.f;
-  vec o = 0.f;
+  f4_t o = {0, 0, 0, 0};
   // runs 0 .. n - 1 of a part, run i's row at base + i * step
   auto add = [&](const Parts &s, int n, int64_t base, int64_t step) {
     for (int i = 0; i < n; i += 64) {
@@ -832,34 +827,46 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
       M = mn;
       l = fmaf(l, al, wave_sum(ml.y * w));
       o *= al;
-      const float *row = s.o + (base + i * step) * D + i0;
-      for (int k = 0; k < c; k += 8) {
-        vec v[8];
+      const float *row = s.o + (base + i * step) * D + col;
+      for (int k = 0; k < c; k += 4 * RL) {
+        f4_t v[4];
+        float wk[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const vec *>(row + min(k + u, c - 1) * step * D);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {      // lanes past c weigh nothing
-          const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k + u));
-          if (wk != 0.f) o += v[u] * wk;
+        for (int u = 0; u < 4; ++u) {
+          const int r = k + u * RL + sub;
+          v[u] = gload_f4(row + min(r, c - 1) * step * D);
+          wk[u] = __shfl(w, r & 63, 64);
+          if (r >= c) wk[u] = 0.f;
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (wk[u] != 0.f) o += v[u] * wk[u];
       }
     }
   };
   if (p.prefix_few) add(p.prefix, p.n_prefix, (int64_t)h * p.prefix_rows + t * a.group + jj, (int64_t)a.heads * p.prefix_rows);
   else add(p.prefix, p.n_prefix, id, (int64_t)a.n_tok * a.n_q);
+  // starts that do not rise leave entries unwritten or written twice: nothing is read by an entry
+  // that is out of bounds
+  if (e.kind != 0 && e.kind != 1) return;
+  e.first = min(max(e.first, 0), p.few_items);
+  e.count = min(max(e.count, 0), p.few_items - e.first);
   if (e.kind == 0) {
     const int rho = min(max(e.place, 0) * a.group + jj, p.few_rows - 1);
     add(p.few, e.count, ((int64_t)e.first * a.heads + h) * p.few_rows + rho, (int64_t)a.heads * p.few_rows);
   } else {
     add(p.many, p.n_many, id, (int64_t)a.n_tok * a.n_q);
   }
+#pragma unroll
+  for (int k = LR; k < 64; k <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], k, 64);
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (lane * E < D) {
-    T *O = static_cast<T *>(a.O) + (int64_t)t * a.o_stride + (int64_t)j * D + lane * E;
+  if (sub == 0) {
+    T *O = static_cast<T *>(a.O) + (int64_t)t * a.o_stride + (int64_t)j * D + col;
     o *= inv;
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<vec *>(O) = o;
-    else if constexpr (E == 2) *reinterpret_cast<uint32_t *>(O) = pack_bf16(o[0], o[1]);
-    else *O = f32_to_bf16(o[0]);
+    if constexpr (sizeof(T) == 4) gstore_f4(O, o);
+    else *reinterpret_cast<uint2 *>(O) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
   }
   if (a.lse && lane == 0) a.lse[id] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
 }
@@ -910,8 +917,8 @@ Cut cut(const PrefixAttendArgs &a, int d, bool bf16) {
     c.prefix_few = rows <= 32;
     if (c.prefix_few) {
       c.prefix_nq = rows <= 16 ? 1 : 2;
-      const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(ceil_div(a.T, RUN_MIN), BLOCKS / a.heads));
-      c.prefix_run = (int)(ceil_div(ceil_div(a.T, runs), RUN_MIN) * RUN_MIN);
+      const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(ceil_div(a.T, RUN_PREFIX), BLOCKS / a.heads));
+      c.prefix_run = (int)(ceil_div(ceil_div(a.T, runs), RUN_PREFIX) * RUN_PREFIX);
       c.n_prefix = (int)ceil_div(a.T, c.prefix_run);
     } else {
       cut_prefix(c, a, d, bf16);
