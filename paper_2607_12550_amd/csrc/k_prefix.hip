@@ -199,7 +199,7 @@ struct Rows {
   using G = Geo<D, T>;
   ju4 q[NQ][G::KS];
   f4_t o[G::FT][NQ];
-  float m[NQ], l[NQ];        // maximum in units of log2 (all lanes of the query), this lane's part of the sum
+  float m[NQ], l[NQ];        // reference in units of log2 (all lanes of the query), this lane's part of the sum
   int seen[NQ];              // tail: tokens the lane's query sees
 
   JOLT_DEV void clear() {
@@ -227,35 +227,44 @@ struct Rows {
       }
     }
   }
-  // Scores s (16 SUBS tokens) into weights, in place, with the running maximum and sum and the
-  // output rescaled where the maximum moved.
+  // Scores s (16 SUBS tokens) into weights, in place.  The reference m of exp2(s c - m) need not
+  // be the running maximum, only near it: it is kept while a lane's weights sum to at most 2^16
+  // (nothing is near overflow then, and a weight's precision does not depend on its size), so
+  // that most tiles need no maximum, no exchange between lanes and no rescaling.  The first tile
+  // (m = -inf gives an infinite sum) and one that outgrows m take the maximum and rescale.
   template <int SUBS>
   JOLT_DEV void softmax(f4_t (&s)[SUBS][NQ], float c) {
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-      float mx = max4(s[0][x]);
+      f4_t p[SUBS];
+      auto weights = [&](float base) {
+        float sum = 0.f;
 #pragma unroll
-      for (int u = 1; u < SUBS; ++u) mx = fmaxf(mx, max4(s[u][x]));
-      mx = fmaxf(m[x], over_groups_max(mx) * c);
-      if (__any(mx > m[x])) {
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][x][i], c, -base));
+            sum += p[u][i];
+          }
+        return sum;
+      };
+      float sum = weights(m[x]);
+      if (__any(!(sum <= 65536.f))) {
+        float mx = max4(s[0][x]);
+#pragma unroll
+        for (int u = 1; u < SUBS; ++u) mx = fmaxf(mx, max4(s[u][x]));
+        mx = fmaxf(m[x], over_groups_max(mx) * c);
         // nothing seen so far: both are -inf, and nothing is there to rescale
         const float al = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[x] - mx);
         l[x] *= al;
 #pragma unroll
         for (int f = 0; f < G::FT; ++f) o[f][x] *= al;
         m[x] = mx;
+        sum = weights(mx == -INFINITY ? 0.f : mx);
       }
-      const float base = mx == -INFINITY ? 0.f : mx;
-      float sum = 0.f;
-#pragma unroll
-      for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[u][x][i], c, -base));
-          s[u][x][i] = p;
-          sum += p;
-        }
       l[x] += sum;
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) s[u][x] = p[u];
     }
   }
   // o += V^T P^T for 16 SUBS tokens whose values stand in LDS; the weights are
@@ -647,14 +656,32 @@ JOLT_DEV void many(const PrefixAttendArgs &a, const ManyArgs &p, int block, Many
   ju4 kr[LOADS], vr[LOADS];
   int pg[LOADS];
   bool ok[LOADS];
-  auto ask_pages = [&](int x) {
+  int64_t off[LOADS];                // prefix: the next tile's rows
+  const int64_t tile_step = (int64_t)G::TILE * src.s_tok * (int)sizeof(T);
+  if constexpr (!TAIL) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) pg[i] = page_of(src, pages, x + i * PASS + lrow, end);
+    for (int i = 0; i < LOADS; ++i) off[i] = row_at(src, 0, h, first + i * PASS + lrow, 0x7fffffff, sizeof(T)).off + piece * 16;
+  }
+  auto ask_pages = [&](int x) {
+    if constexpr (TAIL)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) pg[i] = page_of(src, pages, x + i * PASS + lrow, end);
   };
   auto load = [&](int x) {
+    if constexpr (!TAIL)
+      if (x + G::TILE <= end) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          ok[i] = true;
+          kr[i] = gload_u4(Kb + off[i]);
+          vr[i] = gload_u4(Vb + off[i]);
+          off[i] += tile_step;
+        }
+        return;
+      }
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const RowAt at = row_at(src, pg[i], h, x + i * PASS + lrow, end, sizeof(T));
+      const RowAt at = row_at(src, TAIL ? pg[i] : 0, h, x + i * PASS + lrow, end, sizeof(T));
       ok[i] = at.ok;
       kr[i] = gload_u4(Kb + at.off + piece * 16);
       vr[i] = gload_u4(Vb + at.off + piece * 16);
@@ -665,11 +692,13 @@ JOLT_DEV void many(const PrefixAttendArgs &a, const ManyArgs &p, int block, Many
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int row = i * PASS + lrow;
-      if (!ok[i]) vr[i] = ju4{0, 0, 0, 0};
+      if ((TAIL || x + G::TILE > end) && !ok[i]) vr[i] = ju4{0, 0, 0, 0};
       *reinterpret_cast<ju4 *>(&sm.k[b][row * G::KP + piece * 16]) = kr[i];
       *reinterpret_cast<ju4 *>(&sm.v[b][row * G::VP + piece * 16]) = vr[i];
-      if (piece == 0) sm.there[b][row] = ok[i];
-      if constexpr (TAIL) bad |= nonfinite<T>(vr[i]);
+      if constexpr (TAIL) {
+        if (piece == 0) sm.there[b][row] = ok[i];
+        bad |= nonfinite<T>(vr[i]);
+      }
     }
     if (TAIL && x + G::TILE > seen_all && bad) sm.flag[b] = 1;
   };
@@ -708,7 +737,7 @@ JOLT_DEV void many(const PrefixAttendArgs &a, const ManyArgs &p, int block, Many
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int k = 16 * u + 4 * g + i;
-          const bool in = sm.there[b][k] != 0;
+          const bool in = TAIL ? sm.there[b][k] != 0 : x + k < end;
 #pragma unroll
           for (int q = 0; q < NQ; ++q)
             if (!in || (TAIL && x + k >= R.seen[q])) s[u][q][i] = -INFINITY;
