@@ -825,71 +825,93 @@ struct JoinArgs {
   int32_t n_many;                 // splits of the tails of many's requests
 };
 
-// One wave per row and query head.  A lane takes one run's maximum and sum, so that the weights of
-// 64 runs are known at once and the rows that they weigh are read without waiting for each other:
-// D / 4 lanes a row, 256 / D runs a load, four loads at a time.
-template <int D, class T>
+// WR waves per row and query head, each a share of its runs.  A lane takes one run's reference and
+// sum, so that the weights of 64 runs are known at once and the rows that they weigh are read
+// without waiting for each other: D / 4 lanes a row, 256 / D runs a load, four loads at a time.
+template <int D, class T, int WR>
 __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
   constexpr int LR = D / 4, RL = 64 / LR;      // lanes of a row, rows of a load
+  __shared__ float part[WR == 1 ? 1 : WAVES][D + 2];
   const PrefixAttendArgs &a = p.a;
-  const int lane = threadIdx.x & 63;
-  const int id = (int)(blockIdx.x * WAVES + (threadIdx.x >> 6));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int id = WR == 1 ? (int)blockIdx.x * WAVES + wave : (int)blockIdx.x;
   if (id >= a.n_tok * a.n_q) return;
   const int t = id / a.n_q, j = id - t * a.n_q, h = j / a.group, jj = j - h * a.group;
   const int sub = lane / LR, col = (lane % LR) * 4;
   RowEntry e = p.entries[t];
-  float M = -INFINITY, l = 0.f;
-  f4_t o = {0, 0, 0, 0};
-  // runs 0 .. n - 1 of a part, run i's row at base + i * step
-  auto add = [&](const Parts &s, int n, int64_t base, int64_t step) {
-    for (int i = 0; i < n; i += 64) {
-      const int c = min(64, n - i);
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (lane < c) ml = s.ml[base + (i + lane) * step];
-      float mn = ml.x;
-#pragma unroll
-      for (int k = 32; k >= 1; k >>= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
-      mn = fmaxf(mn, M);
-      // an empty run weighs nothing, whatever its row holds
-      const float w = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - mn);
-      const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
-      M = mn;
-      l = fmaf(l, al, wave_sum(ml.y * w));
-      o *= al;
-      const float *row = s.o + (base + i * step) * D + col;
-      for (int k = 0; k < c; k += 4 * RL) {
-        f4_t v[4];
-        float wk[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int r = k + u * RL + sub;
-          v[u] = gload_f4(row + min(r, c - 1) * step * D);
-          wk[u] = __shfl(w, r & 63, 64);
-          if (r >= c) wk[u] = 0.f;
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (wk[u] != 0.f) o += v[u] * wk[u];
-      }
-    }
-  };
-  if (p.prefix_few) add(p.prefix, p.n_prefix, (int64_t)h * p.prefix_rows + t * a.group + jj, (int64_t)a.heads * p.prefix_rows);
-  else add(p.prefix, p.n_prefix, id, (int64_t)a.n_tok * a.n_q);
   // starts that do not rise leave entries unwritten or written twice: nothing is read by an entry
   // that is out of bounds
   if (e.kind != 0 && e.kind != 1) return;
   e.first = min(max(e.first, 0), p.few_items);
   e.count = min(max(e.count, 0), p.few_items - e.first);
-  if (e.kind == 0) {
-    const int rho = min(max(e.place, 0) * a.group + jj, p.few_rows - 1);
-    add(p.few, e.count, ((int64_t)e.first * a.heads + h) * p.few_rows + rho, (int64_t)a.heads * p.few_rows);
-  } else {
-    add(p.many, p.n_many, id, (int64_t)a.n_tok * a.n_q);
+  // the runs: 0 .. n1 - 1 of the prefix, n1 .. n - 1 of the tail
+  const int64_t step_all = (int64_t)a.n_tok * a.n_q;
+  const int64_t base1 = p.prefix_few ? (int64_t)h * p.prefix_rows + t * a.group + jj : id;
+  const int64_t step1 = p.prefix_few ? (int64_t)a.heads * p.prefix_rows : step_all;
+  const Parts p2 = e.kind == 0 ? p.few : p.many;
+  const int64_t step2 = e.kind == 0 ? (int64_t)a.heads * p.few_rows : step_all;
+  const int64_t base2 = e.kind == 0 ? ((int64_t)e.first * a.heads + h) * p.few_rows + min(max(e.place, 0) * a.group + jj, p.few_rows - 1) : id;
+  const int n1 = p.n_prefix, n = n1 + (e.kind == 0 ? e.count : p.n_many);
+  const int share = WR == 1 ? n : (n + WR - 1) / WR, i0 = WR == 1 ? 0 : wave * share, i1 = min(n, i0 + share);
+  float M = -INFINITY, l = 0.f;
+  f4_t o = {0, 0, 0, 0};
+  for (int i = i0; i < i1; i += 64) {
+    const int c = min(64, i1 - i), mine = i + lane;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < c) ml = mine < n1 ? p.prefix.ml[base1 + mine * step1] : p2.ml[base2 + (mine - n1) * step2];
+    float mn = ml.x;
+#pragma unroll
+    for (int k = 32; k >= 1; k >>= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
+    mn = fmaxf(mn, M);
+    // an empty run weighs nothing, whatever its row holds
+    const float w = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - mn);
+    const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
+    M = mn;
+    l = fmaf(l, al, wave_sum(ml.y * w));
+    o *= al;
+    for (int k = 0; k < c; k += 4 * RL) {
+      f4_t v[4];
+      float wk[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int r = k + u * RL + sub, q = i + min(r, c - 1);
+        const float *row = q < n1 ? p.prefix.o + (base1 + q * step1) * D : p2.o + (base2 + (q - n1) * step2) * D;
+        v[u] = gload_f4(row + col);
+        wk[u] = __shfl(w, r & 63, 64);
+        if (r >= c) wk[u] = 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (wk[u] != 0.f) o += v[u] * wk[u];
+    }
   }
 #pragma unroll
   for (int k = LR; k < 64; k <<= 1)
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], k, 64);
+  if constexpr (WR > 1) {
+    if (sub == 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) part[wave][col + i] = o[i];
+    if (lane == 0) { part[wave][D] = M; part[wave][D + 1] = l; }
+    __syncthreads();
+    if (wave) return;
+    M = part[0][D];
+#pragma unroll
+    for (int w = 1; w < WR; ++w) M = fmaxf(M, part[w][D]);
+    l = 0.f;
+    o = f4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < WR; ++w) {
+      const float mw = part[w][D], lw = part[w][D + 1];
+      if (mw == -INFINITY && lw == 0.f) continue;
+      const float al = __builtin_amdgcn_exp2f(mw - M);
+      l = fmaf(lw, al, l);
+      if (al != 0.f)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(part[w][col + i], al, o[i]);
+    }
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (sub == 0) {
     T *O = static_cast<T *>(a.O) + (int64_t)t * a.o_stride + (int64_t)j * D + col;
@@ -1014,7 +1036,10 @@ hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t
   p.n_few = (int)std::max<int64_t>(1, ceil_div((int64_t)c.few_items * a.heads, WAVES));
   k_runs<D, T><<<p.n_pre + p.n_many + p.n_few, NT, 0, st>>>(p);
   const JoinArgs j{a, pp, pf, pm, entries, c.n_prefix, c.prefix_few, c.few_rows, a.n_tok * a.group, c.few_items, c.n_many};
-  k_join<D, T><<<(int)ceil_div((int64_t)a.n_tok * a.n_q, WAVES), NT, 0, st>>>(j);
+  // four waves a row where one each would leave most of the chip idle
+  const int64_t out_rows = (int64_t)a.n_tok * a.n_q;
+  if (out_rows < 2 * BLOCKS) k_join<D, T, WAVES><<<(int)out_rows, NT, 0, st>>>(j);
+  else k_join<D, T, 1><<<(int)ceil_div(out_rows, WAVES), NT, 0, st>>>(j);
   return hipGetLastError();
 }
 
