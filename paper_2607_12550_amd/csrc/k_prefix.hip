@@ -41,7 +41,7 @@ struct Geo {
   // Bytes of a row in LDS, padded so that what one instruction reads falls in distinct banks and
   // every address is a lane's base plus a constant: 16 rows x 16 bytes of keys; of values 8 rows x
   // 32 bytes by the transposed reads (bf16), rows 4 apart x 64 bytes (fp32).
-  static constexpr int KP = RB + 16, VP = RB + (BF ? 32 : 16);
+  static constexpr int KP = RB + 32, VP = RB + (BF ? 32 : 16);
 };
 
 template <class T>
@@ -234,22 +234,28 @@ struct Rows {
   // (m = -inf gives an infinite sum) and one that outgrows m take the maximum and rescale.
   template <int SUBS>
   JOLT_DEV void softmax(f4_t (&s)[SUBS][NQ], float c) {
+    f4_t p[SUBS][NQ];
+    float sum[NQ];
+    bool far = false;
+    auto weigh = [&](int x) {
+      const float base = m[x] == -INFINITY ? 0.f : m[x];
+      sum[x] = 0.f;
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[u][x][i] = __builtin_amdgcn_exp2f(fmaf(s[u][x][i], c, -base));
+          sum[x] += p[u][x][i];
+        }
+    };
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-      f4_t p[SUBS];
-      auto weights = [&](float base) {
-        float sum = 0.f;
+      weigh(x);
+      far |= !(sum[x] <= 65536.f) || m[x] == -INFINITY;
+    }
+    if (__builtin_expect(__any(far), 0)) {
 #pragma unroll
-        for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][x][i], c, -base));
-            sum += p[u][i];
-          }
-        return sum;
-      };
-      float sum = weights(m[x]);
-      if (__any(!(sum <= 65536.f))) {
+      for (int x = 0; x < NQ; ++x) {
         float mx = max4(s[0][x]);
 #pragma unroll
         for (int u = 1; u < SUBS; ++u) mx = fmaxf(mx, max4(s[u][x]));
@@ -260,11 +266,14 @@ struct Rows {
 #pragma unroll
         for (int f = 0; f < G::FT; ++f) o[f][x] *= al;
         m[x] = mx;
-        sum = weights(mx == -INFINITY ? 0.f : mx);
+        weigh(x);
       }
-      l[x] += sum;
+    }
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u) s[u][x] = p[u];
+    for (int x = 0; x < NQ; ++x) {
+      l[x] += sum[x];
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) s[u][x] = p[u][x];
     }
   }
   // o += V^T P^T for 16 SUBS tokens whose values stand in LDS; the weights are
@@ -591,10 +600,15 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
 }
 
 // ------------------------------------------------------------------------------- many rows
+// The prefix's work of a head, (row tile, tile of keys and values) pairs in that order, is cut into
+// equal pieces of `share` pairs, a workgroup each: a workgroup ends one row tile and starts the
+// next, so that all have the same work whatever the row tiles are.  A row tile's run from its
+// s-th workgroup goes to slab s.  The tails' row tiles are cut into `splits` runs each.
 struct ManyArgs {
-  Parts out;                // [split][packed row][query head]
-  int32_t splits, tiles;    // prefix: row tiles; tails: most row tiles of the call
+  Parts out;                // [slab][packed row][query head]
+  int32_t splits, tiles;    // tails: runs of a row tile, most row tiles of the call; prefix: row tiles
   int32_t limit;            // tails: requests of more rows per head than this
+  int64_t share;            // prefix
 };
 
 template <int D, class T>
@@ -614,162 +628,176 @@ JOLT_DEV void many(const PrefixAttendArgs &a, const ManyArgs &p, int block, Many
   const PrefixSource &src = TAIL ? a.tail : a.prefix;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, g = lane >> 4;
   const int h = block % a.heads, rest = block / a.heads;
-  const int tile = rest % p.tiles, split = rest / p.tiles;
-  int t0, n, len, tail_len = 0, rho0, seen_all = 0x7fffffff;
-  const int32_t *pages = nullptr;
+  // prefix: pairs at .. pairs_end - 1; tails: one run
+  const int kv_tiles = TAIL ? 1 : (a.T + G::TILE - 1) / G::TILE;
+  int64_t at = TAIL ? 0 : rest * p.share;
+  const int64_t pairs_end = TAIL ? 1 : min(at + p.share, (int64_t)p.tiles * kv_tiles);
+  Found found{};
   if constexpr (TAIL) {
-    const int want[1] = {tile};
+    const int want[1] = {rest % p.tiles};
     find_items<1, 1>(a, want, p.limit, RT, nullptr, sm.f);
-    const Found f = sm.f.at[0];
-    if (f.r < 0) return;
-    t0 = f.x.q0;
-    n = f.x.n;
-    tail_len = f.x.len;
-    rho0 = f.idx * RT;
-    // the tile's last row sees most, its first least
-    len = max(0, tail_len - n + min(n, (rho0 + RT - 1) / a.group + 1));
-    seen_all = max(0, tail_len - n + rho0 / a.group + 1);
-    pages = a.table + (int64_t)f.r * a.max_pages;
-  } else {
-    t0 = 0;
-    n = a.n_tok;
-    rho0 = tile * RT;
-    len = a.T;
+    found = sm.f.at[0];
+    if (found.r < 0) return;
   }
-  const int n_rows = n * a.group;
-  const int run = ((len + p.splits - 1) / p.splits + G::TILE - 1) / G::TILE * G::TILE;
-  const int first = split * run, end = min(len, first + run);
-  Rows<D, T, NQ> R;
-  const int rho_w = rho0 + wave * 16 * NQ;
-  R.load(a, h, t0, rho_w, n_rows, n16, g);
-  R.clear();
-  if constexpr (TAIL) {
-#pragma unroll
-    for (int c = 0; c < NQ; ++c) {
-      const int rho = rho_w + 16 * c + n16;
-      R.seen[c] = rho < n_rows ? max(0, tail_len - n + rho / a.group + 1) : 0x7fffffff;
+  while (at < pairs_end) {
+    int t0, n, len, tail_len = 0, rho0, slab, first, end, seen_all = 0x7fffffff;
+    const int32_t *pages = nullptr;
+    if constexpr (TAIL) {
+      t0 = found.x.q0;
+      n = found.x.n;
+      tail_len = found.x.len;
+      rho0 = found.idx * RT;
+      // the tile's last row sees most, its first least
+      len = max(0, tail_len - n + min(n, (rho0 + RT - 1) / a.group + 1));
+      seen_all = max(0, tail_len - n + rho0 / a.group + 1);
+      pages = a.table + (int64_t)found.r * a.max_pages;
+      const int run = ((len + p.splits - 1) / p.splits + G::TILE - 1) / G::TILE * G::TILE;
+      slab = rest / p.tiles;
+      first = slab * run;
+      end = min(len, first + run);
+      at = pairs_end;
+    } else {
+      t0 = 0;
+      n = a.n_tok;
+      const int tile = (int)(at / kv_tiles), k0 = (int)(at - (int64_t)tile * kv_tiles);
+      const int k1 = (int)min((int64_t)kv_tiles, k0 + (pairs_end - at));
+      rho0 = tile * RT;
+      slab = rest - (int)((int64_t)tile * kv_tiles / p.share);
+      first = k0 * G::TILE;
+      end = min(a.T, k1 * G::TILE);
+      at += k1 - k0;
     }
-  }
-  const float c = a.scale * LOG2E;
-  const uint8_t *Kb = static_cast<const uint8_t *>(src.K), *Vb = static_cast<const uint8_t *>(src.V);
-  const int lrow = tid / G::CH, piece = tid % G::CH;
-  ju4 kr[LOADS], vr[LOADS];
-  int pg[LOADS];
-  bool ok[LOADS];
-  int64_t off[LOADS];                // prefix: the next tile's rows
-  const int64_t tile_step = (int64_t)G::TILE * src.s_tok * (int)sizeof(T);
-  if constexpr (!TAIL) {
+    const int n_rows = n * a.group;
+    Rows<D, T, NQ> R;
+    const int rho_w = rho0 + wave * 16 * NQ;
+    R.load(a, h, t0, rho_w, n_rows, n16, g);
+    R.clear();
+    if constexpr (TAIL) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) off[i] = row_at(src, 0, h, first + i * PASS + lrow, 0x7fffffff, sizeof(T)).off + piece * 16;
-  }
-  auto ask_pages = [&](int x) {
-    if constexpr (TAIL)
+      for (int c = 0; c < NQ; ++c) {
+        const int rho = rho_w + 16 * c + n16;
+        R.seen[c] = rho < n_rows ? max(0, tail_len - n + rho / a.group + 1) : 0x7fffffff;
+      }
+    }
+    const float c = a.scale * LOG2E;
+    const uint8_t *Kb = static_cast<const uint8_t *>(src.K), *Vb = static_cast<const uint8_t *>(src.V);
+    const int lrow = tid / G::CH, piece = tid % G::CH;
+    ju4 kr[LOADS], vr[LOADS];
+    int pg[LOADS];
+    bool ok[LOADS];
+    int64_t off[LOADS];                // prefix: the next tile's rows
+    const int64_t tile_step = (int64_t)G::TILE * src.s_tok * (int)sizeof(T);
+    if constexpr (!TAIL) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) pg[i] = page_of(src, pages, x + i * PASS + lrow, end);
-  };
-  auto load = [&](int x) {
-    if constexpr (!TAIL)
-      if (x + G::TILE <= end) {
+      for (int i = 0; i < LOADS; ++i) off[i] = row_at(src, 0, h, first + i * PASS + lrow, 0x7fffffff, sizeof(T)).off + piece * 16;
+    }
+    auto ask_pages = [&](int x) {
+      if constexpr (TAIL)
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          ok[i] = true;
-          kr[i] = gload_u4(Kb + off[i]);
-          vr[i] = gload_u4(Vb + off[i]);
-          off[i] += tile_step;
+        for (int i = 0; i < LOADS; ++i) pg[i] = page_of(src, pages, x + i * PASS + lrow, end);
+    };
+    auto load = [&](int x) {
+      if constexpr (!TAIL)
+        if (x + G::TILE <= end) {
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i) {
+            ok[i] = true;
+            kr[i] = gload_u4(Kb + off[i]);
+            vr[i] = gload_u4(Vb + off[i]);
+            off[i] += tile_step;
+          }
+          return;
         }
-        return;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const RowAt at = row_at(src, TAIL ? pg[i] : 0, h, x + i * PASS + lrow, end, sizeof(T));
+        ok[i] = at.ok;
+        kr[i] = gload_u4(Kb + at.off + piece * 16);
+        vr[i] = gload_u4(Vb + at.off + piece * 16);
       }
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const RowAt at = row_at(src, TAIL ? pg[i] : 0, h, x + i * PASS + lrow, end, sizeof(T));
-      ok[i] = at.ok;
-      kr[i] = gload_u4(Kb + at.off + piece * 16);
-      vr[i] = gload_u4(Vb + at.off + piece * 16);
-    }
-  };
-  auto put = [&](int b, int x) {
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int row = i * PASS + lrow;
-      if ((TAIL || x + G::TILE > end) && !ok[i]) vr[i] = ju4{0, 0, 0, 0};
-      *reinterpret_cast<ju4 *>(&sm.k[b][row * G::KP + piece * 16]) = kr[i];
-      *reinterpret_cast<ju4 *>(&sm.v[b][row * G::VP + piece * 16]) = vr[i];
-      if constexpr (TAIL) {
-        if (piece == 0) sm.there[b][row] = ok[i];
-        bad |= nonfinite<T>(vr[i]);
-      }
-    }
-    if (TAIL && x + G::TILE > seen_all && bad) sm.flag[b] = 1;
-  };
-  if (TAIL && tid < 2) sm.flag[tid] = 0;
-  if (first < end) {
-    ask_pages(first);
-    load(first);
-    ask_pages(first + G::TILE);
-    if (TAIL) __syncthreads();
-    put(0, first);
-    __syncthreads();
-  }
-  for (int x = first, b = 0; x < end; x += G::TILE, b ^= 1) {
-    const bool more = x + G::TILE < end;
-    if (more) {
-      load(x + G::TILE);
-      ask_pages(x + 2 * G::TILE);
-    }
-    const uint8_t *kl = sm.k[b] + n16 * G::KP + 16 * g;
-    uint8_t *vl = sm.v[b];
-    f4_t s[SUBS][NQ];
-#pragma unroll
-    for (int u = 0; u < SUBS; ++u) {
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) s[u][q] = f4_t{0, 0, 0, 0};
-#pragma unroll
-      for (int k = 0; k < G::KS; ++k) {
-        const ju4 ka = *reinterpret_cast<const ju4 *>(kl + 16 * u * G::KP + 64 * k);
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) s[u][q] = product_step<T>(ka, R.q[q][k], s[u][q]);
-      }
-    }
-    if (TAIL || x + G::TILE > end) {
-#pragma unroll
-      for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int k = 16 * u + 4 * g + i;
-          const bool in = TAIL ? sm.there[b][k] != 0 : x + k < end;
-#pragma unroll
-          for (int q = 0; q < NQ; ++q)
-            if (!in || (TAIL && x + k >= R.seen[q])) s[u][q][i] = -INFINITY;
-        }
-    }
-    R.softmax(s, c);
-    if (TAIL && sm.flag[b]) {          // the same for all threads: written before the last barrier
-      R.template add_nonfinite<G::TILE>(vl, x, n16, g);
-      __syncthreads();
+    };
+    auto put = [&](int b, int x) {
+      bool bad = false;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int row = i * PASS + lrow;
-        ju4 *at = reinterpret_cast<ju4 *>(vl + row * G::VP + piece * 16);
-        *at = finite_or_zero<T>(*at);
+        if ((TAIL || x + G::TILE > end) && !ok[i]) vr[i] = ju4{0, 0, 0, 0};
+        *reinterpret_cast<ju4 *>(&sm.k[b][row * G::KP + piece * 16]) = kr[i];
+        *reinterpret_cast<ju4 *>(&sm.v[b][row * G::VP + piece * 16]) = vr[i];
+        if constexpr (TAIL) {
+          if (piece == 0) sm.there[b][row] = ok[i];
+          bad |= nonfinite<T>(vr[i]);
+        }
       }
-      if (tid == 0) sm.flag[b] = 0;
+      if (TAIL && x + G::TILE > seen_all && bad) sm.flag[b] = 1;
+    };
+    if (TAIL && tid < 2) sm.flag[tid] = 0;
+    if (first < end) {
+      ask_pages(first);
+      load(first);
+      ask_pages(first + G::TILE);
+      if (TAIL) __syncthreads();
+      put(0, first);
       __syncthreads();
     }
-    R.values(s, vl, n16, g);
-    if (more) put(b ^ 1, x + G::TILE);
-    __syncthreads();
-  }
+    for (int x = first, b = 0; x < end; x += G::TILE, b ^= 1) {
+      const bool more = x + G::TILE < end;
+      if (more) {
+        load(x + G::TILE);
+        ask_pages(x + 2 * G::TILE);
+      }
+      const uint8_t *kl = sm.k[b] + n16 * G::KP + 16 * g;
+      uint8_t *vl = sm.v[b];
+      // a step's products of all tokens one after the other: no product waits for the one before it
+      f4_t s[SUBS][NQ];
 #pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    const float l = over_groups_sum(R.l[q]);
-    const int rho = rho_w + 16 * q + n16;
-    if (rho < n_rows) {
-      const int t = t0 + rho / a.group, j = h * a.group + rho % a.group;
-      const int64_t row = ((int64_t)split * a.n_tok + t) * a.n_q + j;
+      for (int k = 0; k < G::KS; ++k)
 #pragma unroll
-      for (int f = 0; f < G::FT; ++f) *reinterpret_cast<f4_t *>(p.out.o + row * D + 16 * f + 4 * g) = R.o[f][q];
-      if (g == 0) p.out.ml[row] = make_float2(R.m[q], l);
+        for (int u = 0; u < SUBS; ++u) {
+          const ju4 ka = *reinterpret_cast<const ju4 *>(kl + 16 * u * G::KP + 64 * k);
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) s[u][q] = product_step<T>(ka, R.q[q][k], k == 0 ? f4_t{0, 0, 0, 0} : s[u][q]);
+        }
+      if (TAIL || x + G::TILE > end) {
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = 16 * u + 4 * g + i;
+            const bool in = TAIL ? sm.there[b][k] != 0 : x + k < end;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q)
+              if (!in || (TAIL && x + k >= R.seen[q])) s[u][q][i] = -INFINITY;
+          }
+      }
+      R.softmax(s, c);
+      if (TAIL && sm.flag[b]) {          // the same for all threads: written before the last barrier
+        R.template add_nonfinite<G::TILE>(vl, x, n16, g);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const int row = i * PASS + lrow;
+          ju4 *at = reinterpret_cast<ju4 *>(vl + row * G::VP + piece * 16);
+          *at = finite_or_zero<T>(*at);
+        }
+        if (tid == 0) sm.flag[b] = 0;
+        __syncthreads();
+      }
+      R.values(s, vl, n16, g);
+      if (more) put(b ^ 1, x + G::TILE);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const float l = over_groups_sum(R.l[q]);
+      const int rho = rho_w + 16 * q + n16;
+      if (rho < n_rows) {
+        const int t = t0 + rho / a.group, j = h * a.group + rho % a.group;
+        const int64_t row = ((int64_t)slab * a.n_tok + t) * a.n_q + j;
+#pragma unroll
+        for (int f = 0; f < G::FT; ++f) *reinterpret_cast<f4_t *>(p.out.o + row * D + 16 * f + 4 * g) = R.o[f][q];
+        if (g == 0) p.out.ml[row] = make_float2(R.m[q], l);
+      }
     }
   }
 }
@@ -821,6 +849,8 @@ struct JoinArgs {
   Parts prefix, few, many;
   const RowEntry *entries;
   int32_t n_prefix, prefix_few;   // runs of the prefix; laid out as few's
+  int32_t prefix_rt, kv_tiles;    // or as many's: rows of a row tile, pairs of it and of a workgroup
+  int64_t share;
   int32_t few_rows, prefix_rows, few_items;
   int32_t n_many;                 // splits of the tails of many's requests
 };
@@ -851,7 +881,13 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
   const Parts p2 = e.kind == 0 ? p.few : p.many;
   const int64_t step2 = e.kind == 0 ? (int64_t)a.heads * p.few_rows : step_all;
   const int64_t base2 = e.kind == 0 ? ((int64_t)e.first * a.heads + h) * p.few_rows + min(max(e.place, 0) * a.group + jj, p.few_rows - 1) : id;
-  const int n1 = p.n_prefix, n = n1 + (e.kind == 0 ? e.count : p.n_many);
+  int n1 = p.n_prefix;
+  if (!p.prefix_few && n1 > 0) {
+    const int tile = (t * a.group + jj) / p.prefix_rt;
+    const int64_t at = (int64_t)tile * p.kv_tiles;
+    n1 = (int)((at + p.kv_tiles - 1) / p.share - at / p.share) + 1;
+  }
+  const int n = n1 + (e.kind == 0 ? e.count : p.n_many);
   const int share = WR == 1 ? n : (n + WR - 1) / WR, i0 = WR == 1 ? 0 : wave * share, i1 = min(n, i0 + share);
   float M = -INFINITY, l = 0.f;
   f4_t o = {0, 0, 0, 0};
@@ -859,6 +895,17 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
     const int c = min(64, i1 - i), mine = i + lane;
     float2 ml = make_float2(-INFINITY, 0.f);
     if (lane < c) ml = mine < n1 ? p.prefix.ml[base1 + mine * step1] : p2.ml[base2 + (mine - n1) * step2];
+    // the rows of 4 RL runs: none waits for a weight
+    f4_t v[4];
+    auto rows = [&](int k) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int q = i + min(k + u * RL + sub, c - 1);
+        const float *row = q < n1 ? p.prefix.o + (base1 + q * step1) * D : p2.o + (base2 + (q - n1) * step2) * D;
+        v[u] = gload_f4(row + col);
+      }
+    };
+    rows(0);
     float mn = ml.x;
 #pragma unroll
     for (int k = 32; k >= 1; k >>= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
@@ -870,19 +917,13 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
     l = fmaf(l, al, wave_sum(ml.y * w));
     o *= al;
     for (int k = 0; k < c; k += 4 * RL) {
-      f4_t v[4];
-      float wk[4];
+      if (k) rows(k);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int r = k + u * RL + sub, q = i + min(r, c - 1);
-        const float *row = q < n1 ? p.prefix.o + (base1 + q * step1) * D : p2.o + (base2 + (q - n1) * step2) * D;
-        v[u] = gload_f4(row + col);
-        wk[u] = __shfl(w, r & 63, 64);
-        if (r >= c) wk[u] = 0.f;
+        const int r = k + u * RL + sub;
+        float wk = __shfl(w, r & 63, 64);
+        if (r < c && wk != 0.f) o += v[u] * wk;
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (wk[u] != 0.f) o += v[u] * wk[u];
     }
   }
 #pragma unroll
@@ -926,7 +967,9 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
 // How a call is cut, from its sizes alone (the workspace depends on it too).
 struct Cut {
   bool prefix_few = false, tails_many = false;
-  int prefix_nq = 1, prefix_run = 0, n_prefix = 0, prefix_tiles = 0;   // of k_few / k_many
+  int prefix_nq = 1, prefix_run = 0, n_prefix = 0;
+  int prefix_tiles = 0, prefix_groups = 0, kv_tiles = 0;     // of many()
+  int64_t share = 1;
   int few_nq = 1, few_items = 0, few_rows = 0, limit = 0;
   int many_nq = 1, many_tiles = 0, n_many = 0;
   size_t off_po, off_pm, off_fo, off_fm, off_mo, off_mm, off_entries, total;
@@ -935,27 +978,33 @@ constexpr int BLOCKS = 512;        // workgroups that fill the chip: two a CU
 
 int64_t ceil_div(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
-// Row tiles and splits of the prefix for many(): the cheapest by a model in us.  A workgroup that
-// has its CU to itself takes about `tile` us a tile of keys and values (the matrix work, and a
-// part that waits for memory and LDS) and 4 us to start and end; two on a CU take 1.5 times as
-// long as one; every split's output is written and read once more, at about 4 MB a us.
+// Row tiles of the prefix for many() and the workgroups of a head: the cheapest by a model in us.  A
+// workgroup that has its CU to itself takes about `tile` us a tile of keys and values (the matrix
+// work, and a part that waits for memory and LDS) and 4 us to start and end a row tile; two on a
+// CU take 1.5 times as long as one; every run's output is written and read once more, at about
+// 4 MB a us.
 void cut_prefix(Cut &c, const PrefixAttendArgs &a, int d, bool bf16) {
   const int64_t rows = (int64_t)a.n_tok * a.group, tokens = bf16 ? 64 : 32;
   const double out = (double)a.n_tok * a.n_q * d * 8 / 4e6;
   double best = 0;
   c.n_prefix = 0;
+  c.kv_tiles = (int)ceil_div(a.T, tokens);
   for (int nq = 1; nq <= 2; ++nq) {
-    const int64_t tiles = ceil_div(rows, 64 * nq);
+    const int64_t tiles = ceil_div(rows, 64 * nq), pairs = tiles * c.kv_tiles;
     const double tile = 0.3 + (bf16 ? 0.9 : 3.4) * d / 128 * nq / 2;
-    for (int s = 1; s <= 64 && (s == 1 || a.T >= tokens * s); ++s) {
-      const int64_t n = a.heads * tiles * s, rem = n % BLOCKS;
-      const double rounds = 1.5 * (n / BLOCKS) + (rem == 0 ? 0 : rem <= BLOCKS / 2 ? 1 : 1.5);
-      const double cost = rounds * (tile * ceil_div(ceil_div(a.T, s), tokens) + 4) + s * out;
+    for (int64_t groups = BLOCKS; groups >= 32; groups /= 2) {
+      // more than the chip holds at once only where there are more heads than that
+      const int64_t share = ceil_div(pairs, std::max<int64_t>(1, groups / a.heads)), n = a.heads * ceil_div(pairs, share);
+      const double slabs = (double)share >= c.kv_tiles ? 1 + (double)(c.kv_tiles - 1) / share : (double)c.kv_tiles / share;
+      const double rounds = 1.5 * (n / BLOCKS) + (n % BLOCKS == 0 ? 0 : n % BLOCKS <= BLOCKS / 2 ? 1 : 1.5);
+      const double cost = rounds * (tile * share + 4 * ceil_div(share + c.kv_tiles - 1, c.kv_tiles)) + slabs * out;
       if (c.n_prefix == 0 || cost < best) {
         best = cost;
-        c.n_prefix = s;
         c.prefix_nq = nq;
         c.prefix_tiles = (int)tiles;
+        c.share = share;
+        c.prefix_groups = (int)ceil_div(pairs, share);
+        c.n_prefix = (int)ceil_div(c.kv_tiles - 1, share) + 1;   // most workgroups of a row tile
       }
     }
   }
@@ -1021,12 +1070,12 @@ hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t
     p.pre_role = c.prefix_nq == 1 ? ROLE_FEW1 : ROLE_FEW2;
     p.n_pre = c.n_prefix * a.heads;
   } else if (a.T > 0) {
-    p.pre_many = ManyArgs{pp, c.n_prefix, c.prefix_tiles, 0};
+    p.pre_many = ManyArgs{pp, 1, c.prefix_tiles, 0, c.share};
     p.pre_role = c.prefix_nq == 1 ? ROLE_MANY1 : ROLE_MANY2;
-    p.n_pre = c.n_prefix * c.prefix_tiles * a.heads;
+    p.n_pre = c.prefix_groups * a.heads;
   }
   if (c.tails_many) {
-    p.many = ManyArgs{pm, c.n_many, c.many_tiles, c.limit};
+    p.many = ManyArgs{pm, c.n_many, c.many_tiles, c.limit, 1};
     p.many_role = c.many_nq == 1 ? ROLE_MANY1 : ROLE_MANY2;
     p.n_many = c.n_many * c.many_tiles * a.heads;
   }
@@ -1035,7 +1084,7 @@ hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t
   p.few_role = c.few_nq == 1 ? ROLE_FEW1 : ROLE_FEW2;
   p.n_few = (int)std::max<int64_t>(1, ceil_div((int64_t)c.few_items * a.heads, WAVES));
   k_runs<D, T><<<p.n_pre + p.n_many + p.n_few, NT, 0, st>>>(p);
-  const JoinArgs j{a, pp, pf, pm, entries, c.n_prefix, c.prefix_few, c.few_rows, a.n_tok * a.group, c.few_items, c.n_many};
+  const JoinArgs j{a, pp, pf, pm, entries, c.n_prefix, c.prefix_few, 64 * c.prefix_nq, c.kv_tiles, c.share, c.few_rows, a.n_tok * a.group, c.few_items, c.n_many};
   // four waves a row where one each would leave most of the chip idle
   const int64_t out_rows = (int64_t)a.n_tok * a.n_q;
   if (out_rows < 2 * BLOCKS) k_join<D, T, WAVES><<<(int)out_rows, NT, 0, st>>>(j);
