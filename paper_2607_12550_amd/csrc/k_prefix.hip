@@ -899,11 +899,12 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
     f4_t v[4];
     auto rows = [&](int k) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int q = i + min(k + u * RL + sub, c - 1);
-        const float *row = q < n1 ? p.prefix.o + (base1 + q * step1) * D : p2.o + (base2 + (q - n1) * step2) * D;
-        v[u] = gload_f4(row + col);
-      }
+      for (int u = 0; u < 4; ++u)
+        if (k + u * RL < c) {
+          const int q = i + min(k + u * RL + sub, c - 1);
+          const float *row = q < n1 ? p.prefix.o + (base1 + q * step1) * D : p2.o + (base2 + (q - n1) * step2) * D;
+          v[u] = gload_f4(row + col);
+        }
     };
     rows(0);
     float mn = ml.x;
@@ -982,7 +983,7 @@ int64_t ceil_div(int64_t x, int64_t y) { return (x + y - 1) / y; }
 // workgroup that has its CU to itself takes about `tile` us a tile of keys and values (the matrix
 // work, and a part that waits for memory and LDS) and 4 us to start and end a row tile; two on a
 // CU take 1.5 times as long as one; every run's output is written and read once more, at about
-// 4 MB a us.
+// 4 MB a us and 0.1 us a run of a row.
 void cut_prefix(Cut &c, const PrefixAttendArgs &a, int d, bool bf16) {
   const int64_t rows = (int64_t)a.n_tok * a.group, tokens = bf16 ? 64 : 32;
   const double out = (double)a.n_tok * a.n_q * d * 8 / 4e6;
@@ -992,12 +993,11 @@ void cut_prefix(Cut &c, const PrefixAttendArgs &a, int d, bool bf16) {
   for (int nq = 1; nq <= 2; ++nq) {
     const int64_t tiles = ceil_div(rows, 64 * nq), pairs = tiles * c.kv_tiles;
     const double tile = 0.3 + (bf16 ? 0.9 : 3.4) * d / 128 * nq / 2;
-    for (int64_t groups = BLOCKS; groups >= 32; groups /= 2) {
-      // more than the chip holds at once only where there are more heads than that
-      const int64_t share = ceil_div(pairs, std::max<int64_t>(1, groups / a.heads)), n = a.heads * ceil_div(pairs, share);
+    for (int64_t of = std::max<int64_t>(1, BLOCKS / a.heads); of >= 1; of = of * 7 / 8) {   // workgroups of a head
+      const int64_t share = ceil_div(pairs, of), n = a.heads * ceil_div(pairs, share);
       const double slabs = (double)share >= c.kv_tiles ? 1 + (double)(c.kv_tiles - 1) / share : (double)c.kv_tiles / share;
       const double rounds = 1.5 * (n / BLOCKS) + (n % BLOCKS == 0 ? 0 : n % BLOCKS <= BLOCKS / 2 ? 1 : 1.5);
-      const double cost = rounds * (tile * share + 4 * ceil_div(share + c.kv_tiles - 1, c.kv_tiles)) + slabs * out;
+      const double cost = rounds * (tile * share + 4 * (1 + (double)(share - 1) / c.kv_tiles)) + slabs * (out + 0.1);
       if (c.n_prefix == 0 || cost < best) {
         best = cost;
         c.prefix_nq = nq;
