@@ -469,22 +469,25 @@ def page_desc(*, dtype, n_heads, page_size, d, n_pages, stride_page, stride_head
 
 
 _TORCH_TYPES = {JOLT_F32: torch.float32, JOLT_BF16: torch.bfloat16}
+_INT32 = torch.int32
 
 
-def _int32s(name, x, n):
-    """Address of a contiguous int32 tensor of n elements."""
-    if x.dtype != torch.int32 or x.numel() != n or not x.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements")
-    return x.data_ptr()
+def _int32s(*checked):
+    """Addresses of contiguous int32 tensors, given as (tensor, elements, name)."""
+    for x, n, name in checked:
+        if x.dtype is not _INT32 or x.numel() != n or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements")
+    return [x.data_ptr() for x, _, _ in checked]
 
 
-def _rows(name, x, dtype, n_heads, d):
-    """Token and head strides of a [tokens, heads, d] tensor whose features are contiguous."""
+def _rows(name, x, n, dtype, n_heads, d):
+    """Token and head strides of an [n, heads, d] tensor whose features are contiguous."""
     want = _TORCH_TYPES.get(dtype)
-    if x.dtype != want or x.dim() != 3 or x.shape[1:] != (n_heads, d) or x.stride(2) != 1:
-        raise ValueError(f"{name} must be [tokens, {n_heads}, {d}] of type {want} with contiguous features")
+    if x.dtype is not want or x.shape != (n, n_heads, d) or x.stride(2) != 1:
+        raise ValueError(f"{name} must be [{n}, {n_heads}, {d}] of type {want} with contiguous features")
     # the stride of an axis of one element is never used: it may be anything
-    return RowStrides(x.stride(0) if x.shape[0] > 1 else 0, x.stride(1) if n_heads > 1 else 0)
+    token, head, _ = x.stride()
+    return RowStrides(token if n > 1 else 0, head if n_heads > 1 else 0)
 
 
 def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, kv_len, q_start, slots, positions,
@@ -492,28 +495,29 @@ def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, k
     """Block tables and slot maps of a step from the requests' lengths (device int32 tensors):
     have, add, kv_len [n_req]; q_start [n_req + 1]; table [n_req, max_pages]; slots, positions
     [n_tok]; n_free, n_free_out [1]; info [4]."""
-    n, n_tok = have.numel(), slots.numel()
+    n, n_tok, cap = have.numel(), slots.numel(), free_pages.numel()
     if table.dim() != 2 or table.shape[0] != n:
         raise ValueError("table must be [n_req, max_pages]")
-    _check(lib.jolt_page_plan(ctx, C.byref(pages), n, _int32s("have", have, n), _int32s("add", add, n),
-                              _int32s("free_pages", free_pages, free_pages.numel()), free_pages.numel(),
-                              _int32s("n_free", n_free, 1), _int32s("table", table, table.numel()), table.shape[1], n_tok,
-                              _int32s("kv_len", kv_len, n), _int32s("q_start", q_start, n + 1),
-                              _int32s("slots", slots, n_tok), _int32s("positions", positions, n_tok),
-                              _int32s("n_free_out", n_free_out, 1), _int32s("info", info, 4), _stream(stream)))
+    columns = table.shape[1]
+    h, ad, fr, nf, tb, kv, qs, sl, po, no, inf = _int32s(
+        (have, n, "have"), (add, n, "add"), (free_pages, cap, "free_pages"), (n_free, 1, "n_free"), (table, n * columns, "table"),
+        (kv_len, n, "kv_len"), (q_start, n + 1, "q_start"), (slots, n_tok, "slots"), (positions, n_tok, "positions"),
+        (n_free_out, 1, "n_free_out"), (info, 4, "info"))
+    _check(lib.jolt_page_plan(ctx, pages, n, h, ad, fr, cap, nf, tb, columns, n_tok, kv, qs, sl, po, no, inf, _stream(stream)))
 
 
 def jolt_page_append(ctx, pages: PageDesc, K, V, slots, K_pages, V_pages, positions=None, rope=None, stream=None) -> None:
     """Writes the rows K, V [n_tok, n_heads, d] into their slots of the pools; rope: None, or
     (base, position_offset) to rotate the keys at positions + position_offset."""
-    n = slots.numel()
-    ks, vs = _rows("K", K, pages.dtype, pages.n_heads, pages.d), _rows("V", V, pages.dtype, pages.n_heads, pages.d)
-    if K.shape[0] != n or V.shape[0] != n:
-        raise ValueError("K, V and slots must have the same number of rows")
-    r = None if rope is None else C.byref(Rope(float(rope[0]), int(rope[1]), 0))
-    _check(lib.jolt_page_append(ctx, C.byref(pages), n, _int32s("slots", slots, n),
-                                0 if positions is None else _int32s("positions", positions, n), r, K.data_ptr(),
-                                C.byref(ks), V.data_ptr(), C.byref(vs), _addr(K_pages), _addr(V_pages), _stream(stream)))
+    n, dtype, heads, d = slots.numel(), pages.dtype, pages.n_heads, pages.d
+    ks, vs = _rows("K", K, n, dtype, heads, d), _rows("V", V, n, dtype, heads, d)
+    if positions is None:
+        (sl,), po = _int32s((slots, n, "slots")), 0
+    else:
+        sl, po = _int32s((slots, n, "slots"), (positions, n, "positions"))
+    r = None if rope is None else Rope(float(rope[0]), int(rope[1]), 0)
+    _check(lib.jolt_page_append(ctx, pages, n, sl, po, r, K.data_ptr(), ks, V.data_ptr(), vs, _addr(K_pages), _addr(V_pages),
+                                _stream(stream)))
 
 
 def jolt_prefix_attend_workspace_size(n_req: int, n_tok: int, n_q: int, prefix=None, pages=None, max_pages: int = 0,
@@ -537,26 +541,31 @@ def jolt_prefix_attend(ctx, Q, O, q_start, kv_len, scale: float, ws, prefix=None
     desc = pages if pages is not None else prefix
     if desc is None:
         raise ValueError("a prefix or pages are needed")
-    if Q.dim() != 3 or Q.shape != O.shape or Q.shape[2] != desc.d:
-        raise ValueError(f"Q and O must be [n_tok, n_q, {desc.d}]")
-    n_tok, n_q, d = Q.shape
-    want = _TORCH_TYPES.get(desc.dtype)
+    shape, d, want = Q.shape, desc.d, _TORCH_TYPES.get(desc.dtype)
+    if len(shape) != 3 or shape[2] != d or O.shape != shape:
+        raise ValueError(f"Q and O must be [n_tok, n_q, {d}]")
+    n_tok, n_q, _ = shape
+    strides = []
     for name, x in (("Q", Q), ("O", O)):
-        if x.dtype != want or x.stride(2) != 1 or (n_q > 1 and x.stride(1) != d):
+        token, head, one = x.stride()
+        if x.dtype is not want or one != 1 or (head != d and n_q > 1):
             raise ValueError(f"{name} must be of type {want} with contiguous rows")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_tok, n_q) or not lse.is_contiguous()):
+        strides.append(token if n_tok > 1 else n_q * d)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n_tok, n_q) or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous fp32 tensor [n_tok, n_q]")
-    max_pages, tab, lens = 0, 0, 0
+    columns, tab, lens = 0, 0, 0
     if pages is not None:
         if table.dim() != 2 or table.shape[0] != n_req:
             raise ValueError("table must be [n_req, max_pages]")
-        max_pages, tab, lens = table.shape[1], _int32s("table", table, table.numel()), _int32s("kv_len", kv_len, n_req)
-    b = AttendBatch(n_req, n_tok, n_q, max_pages, max_new, 0, *(x.stride(0) if n_tok > 1 else n_q * d for x in (Q, O)))
+        columns = table.shape[1]
+        starts, tab, lens = _int32s((q_start, n_req + 1, "q_start"), (table, n_req * columns, "table"), (kv_len, n_req, "kv_len"))
+    else:
+        starts, = _int32s((q_start, n_req + 1, "q_start"))
+    b = AttendBatch(n_req, n_tok, n_q, columns, max_new, 0, *strides)
     wsb = ws_bytes if ws_bytes is not None else (ws.numel() * ws.element_size())
-    _check(lib.jolt_prefix_attend(ctx, None if prefix is None else C.byref(prefix), _addr(K_prefix), _addr(V_prefix), layer,
-                                  None if pages is None else C.byref(pages), _addr(K_pages), _addr(V_pages), tab, C.byref(b),
-                                  _int32s("q_start", q_start, n_req + 1), lens, Q.data_ptr(), float(scale), O.data_ptr(),
-                                  _addr(lse), _addr(ws), wsb, _stream(stream)))
+    _check(lib.jolt_prefix_attend(ctx, prefix, _addr(K_prefix), _addr(V_prefix), layer, pages, _addr(K_pages), _addr(V_pages), tab, b,
+                                  starts, lens, Q.data_ptr(), float(scale), O.data_ptr(), _addr(lse), _addr(ws), wsb,
+                                  _stream(stream)))
 
 
 def jolt_debug_export(ctx, what: int, cell: int, dst, stream=None) -> None:

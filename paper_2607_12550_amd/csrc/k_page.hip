@@ -15,7 +15,10 @@ constexpr int NT = 256, WAVES = NT / 64;
 // Latency bounds it: the sums are short (at most 4096 requests) and every workgroup forms them
 // for itself, which takes one launch instead of a scan and a second kernel that waits for it.
 // Workgroup 0 writes the per-request outputs.
-constexpr int PLAN_ROWS = 4 * NT;   // packed rows of a workgroup
+//
+// A thread takes four rows in a row: one bisection for the first, the others step on from it, and
+// their page reads are under way together.
+constexpr int PLAN_STEP = 4, PLAN_ROWS = PLAN_STEP * NT;   // packed rows of a thread, of a workgroup
 
 JOLT_DEV int64_t wave_scan(int64_t v, int lane) {   // inclusive
 #pragma unroll
@@ -30,6 +33,7 @@ __global__ void __launch_bounds__(NT) k_page_plan(const PagePlanArgs a) {
   extern __shared__ int32_t lds[];
   int32_t *start = lds;                    // [n_req + 1] first packed row
   int32_t *first = lds + a.n_req + 1;      // [n_req] first new page of the call
+  int32_t *held = first + a.n_req;         // [n_req] have
   __shared__ int64_t tot[2][WAVES];
   __shared__ int bad[WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -72,6 +76,7 @@ __global__ void __launch_bounds__(NT) k_page_plan(const PagePlanArgs a) {
     if (!why) {
       start[r] = (int)row0;
       first[r] = (int)page0;
+      held[r] = h;
       row0 += n;
       page0 += (((int64_t)h + n + mask) >> sh) - (((int64_t)h + mask) >> sh);
     }
@@ -86,26 +91,42 @@ __global__ void __launch_bounds__(NT) k_page_plan(const PagePlanArgs a) {
   }
   if (!why && tid == 0) start[a.n_req] = (int)all_rows;
   __syncthreads();
-  const int t0 = blockIdx.x * PLAN_ROWS;
-  for (int t = t0 + tid; t < min(t0 + PLAN_ROWS, a.n_tok); t += NT) {
-    int slot = -1, pos = -1;
-    if (!why && t < all_rows) {
-      int lo = 0, hi = a.n_req;            // start[lo] <= t < start[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= t) lo = mid; else hi = mid;
-      }
-      const int have = a.have[lo];
-      pos = have + (t - start[lo]);
-      const int j = pos >> sh, fresh = j - (int)(((int64_t)have + mask) >> sh);
-      int32_t *entry = a.table + (int64_t)lo * a.max_pages + j;
-      const int page = fresh >= 0 ? a.free_pages[n_free - 1 - (first[lo] + fresh)] : *entry;
-      if ((pos & mask) == 0) *entry = page;
-      if ((uint32_t)page < (uint32_t)a.n_pages) slot = (page << sh) + (pos & mask);
+  const int t0 = (blockIdx.x * NT + tid) * PLAN_STEP;
+  if (t0 >= a.n_tok) return;
+  int slot[PLAN_STEP], pos[PLAN_STEP], req[PLAN_STEP], page[PLAN_STEP];
+  int lo = 0;
+  if (!why && t0 < all_rows) {
+    int hi = a.n_req;                      // start[lo] <= t0 < start[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (start[mid] <= t0) lo = mid; else hi = mid;
     }
-    a.slots[t] = slot;
-    a.positions[t] = pos;
   }
+#pragma unroll
+  for (int i = 0; i < PLAN_STEP; ++i) {
+    const int t = t0 + i;
+    slot[i] = pos[i] = -1;
+    req[i] = -1;
+    if (why || t >= all_rows) continue;
+    while (start[lo + 1] <= t) ++lo;       // ends: t < all_rows = start[n_req]
+    const int have = held[lo];
+    req[i] = lo;
+    pos[i] = have + (t - start[lo]);
+    const int j = pos[i] >> sh, fresh = j - (int)(((int64_t)have + mask) >> sh);
+    page[i] = fresh >= 0 ? a.free_pages[n_free - 1 - (first[lo] + fresh)] : a.table[(int64_t)lo * a.max_pages + j];
+  }
+#pragma unroll
+  for (int i = 0; i < PLAN_STEP; ++i)
+    if (req[i] >= 0) {
+      if ((pos[i] & mask) == 0) a.table[(int64_t)req[i] * a.max_pages + (pos[i] >> sh)] = page[i];
+      if ((uint32_t)page[i] < (uint32_t)a.n_pages) slot[i] = (page[i] << sh) + (pos[i] & mask);
+    }
+#pragma unroll
+  for (int i = 0; i < PLAN_STEP; ++i)
+    if (t0 + i < a.n_tok) {
+      a.slots[t0 + i] = slot[i];
+      a.positions[t0 + i] = pos[i];
+    }
 }
 
 // ------------------------------------------------------------------------------- append
@@ -189,7 +210,7 @@ hipError_t append(const PageAppendArgs &a, int dtype, hipStream_t st) {
 
 hipError_t launch_page_plan(const PagePlanArgs &a, hipStream_t st) {
   const int grid = (a.n_tok + PLAN_ROWS - 1) / PLAN_ROWS;
-  k_page_plan<<<grid, NT, (2 * a.n_req + 1) * sizeof(int32_t), st>>>(a);
+  k_page_plan<<<grid, NT, (3 * a.n_req + 1) * sizeof(int32_t), st>>>(a);
   return hipGetLastError();
 }
 

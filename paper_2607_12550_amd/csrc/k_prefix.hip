@@ -855,19 +855,20 @@ struct JoinArgs {
   int32_t n_many;                 // splits of the tails of many's requests
 };
 
-// WR waves per row and query head, each a share of its runs.  A lane takes one run's reference and
-// sum, so that the weights of 64 runs are known at once and the rows that they weigh are read
-// without waiting for each other: D / 4 lanes a row, 256 / D runs a load, four loads at a time.
-template <int D, class T, int WR>
+// LW lanes of a wave per row and query head or, BLOCK, the four waves of a workgroup, each a share
+// of its runs.  A lane takes one run's reference and sum, so that the weights of LW runs are known
+// at once, and the rows that they weigh (D / 4 lanes each, several under way) are read without
+// waiting for them.
+template <int D, class T, int LW, bool BLOCK>
 __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
-  constexpr int LR = D / 4, RL = 64 / LR;      // lanes of a row, rows of a load
-  __shared__ float part[WR == 1 ? 1 : WAVES][D + 2];
+  constexpr int LR = D / 4, RL = LW / LR, AHEAD = RL == 1 ? 8 : 4;   // lanes of a run's row, rows of a load, loads under way
+  static_assert(!BLOCK || LW == 64, "whole waves share a row");
+  __shared__ float part[BLOCK ? WAVES : 1][D + 2];
   const PrefixAttendArgs &a = p.a;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int id = WR == 1 ? (int)blockIdx.x * WAVES + wave : (int)blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, gl = lane % LW, sub = gl / LR, col = 4 * (gl % LR);
+  const int id = BLOCK ? (int)blockIdx.x : (int)blockIdx.x * (NT / LW) + (int)threadIdx.x / LW;
   if (id >= a.n_tok * a.n_q) return;
   const int t = id / a.n_q, j = id - t * a.n_q, h = j / a.group, jj = j - h * a.group;
-  const int sub = lane / LR, col = (lane % LR) * 4;
   RowEntry e = p.entries[t];
   // starts that do not rise leave entries unwritten or written twice: nothing is read by an entry
   // that is out of bounds
@@ -883,55 +884,55 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
   const int64_t base2 = e.kind == 0 ? ((int64_t)e.first * a.heads + h) * p.few_rows + min(max(e.place, 0) * a.group + jj, p.few_rows - 1) : id;
   int n1 = p.n_prefix;
   if (!p.prefix_few && n1 > 0) {
-    const int tile = (t * a.group + jj) / p.prefix_rt;
-    const int64_t at = (int64_t)tile * p.kv_tiles;
+    const int64_t at = (int64_t)((t * a.group + jj) / p.prefix_rt) * p.kv_tiles;
     n1 = (int)((at + p.kv_tiles - 1) / p.share - at / p.share) + 1;
   }
   const int n = n1 + (e.kind == 0 ? e.count : p.n_many);
-  const int share = WR == 1 ? n : (n + WR - 1) / WR, i0 = WR == 1 ? 0 : wave * share, i1 = min(n, i0 + share);
+  const int share = BLOCK ? (n + WAVES - 1) / WAVES : n, i0 = BLOCK ? wave * share : 0, i1 = min(n, i0 + share);
   float M = -INFINITY, l = 0.f;
   f4_t o = {0, 0, 0, 0};
-  for (int i = i0; i < i1; i += 64) {
-    const int c = min(64, i1 - i), mine = i + lane;
+  for (int i = i0; i < i1; i += LW) {
+    const int c = min(LW, i1 - i), mine = i + gl;
     float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < c) ml = mine < n1 ? p.prefix.ml[base1 + mine * step1] : p2.ml[base2 + (mine - n1) * step2];
-    // the rows of 4 RL runs: none waits for a weight
-    f4_t v[4];
+    if (gl < c) ml = mine < n1 ? p.prefix.ml[base1 + mine * step1] : p2.ml[base2 + (mine - n1) * step2];
+    f4_t v[AHEAD];
     auto rows = [&](int k) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < AHEAD; ++u)
         if (k + u * RL < c) {
           const int q = i + min(k + u * RL + sub, c - 1);
-          const float *row = q < n1 ? p.prefix.o + (base1 + q * step1) * D : p2.o + (base2 + (q - n1) * step2) * D;
-          v[u] = gload_f4(row + col);
+          v[u] = gload_f4((q < n1 ? p.prefix.o + (base1 + q * step1) * D : p2.o + (base2 + (q - n1) * step2) * D) + col);
         }
     };
     rows(0);
     float mn = ml.x;
 #pragma unroll
-    for (int k = 32; k >= 1; k >>= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
+    for (int k = LW / 2; k >= 1; k >>= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
     mn = fmaxf(mn, M);
     // an empty run weighs nothing, whatever its row holds
     const float w = ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - mn);
     const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
     M = mn;
-    l = fmaf(l, al, wave_sum(ml.y * w));
+    float sum = ml.y * w;
+#pragma unroll
+    for (int k = LW / 2; k >= 1; k >>= 1) sum += __shfl_xor(sum, k, 64);
+    l = fmaf(l, al, sum);
     o *= al;
-    for (int k = 0; k < c; k += 4 * RL) {
+    for (int k = 0; k < c; k += AHEAD * RL) {
       if (k) rows(k);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < AHEAD; ++u) {
         const int r = k + u * RL + sub;
-        float wk = __shfl(w, r & 63, 64);
+        const float wk = __shfl(w, (lane & ~(LW - 1)) + (r & (LW - 1)), 64);
         if (r < c && wk != 0.f) o += v[u] * wk;
       }
     }
   }
 #pragma unroll
-  for (int k = LR; k < 64; k <<= 1)
+  for (int k = LR; k < LW; k <<= 1)
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], k, 64);
-  if constexpr (WR > 1) {
+  if constexpr (BLOCK) {
     if (sub == 0)
 #pragma unroll
       for (int i = 0; i < 4; ++i) part[wave][col + i] = o[i];
@@ -940,11 +941,11 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
     if (wave) return;
     M = part[0][D];
 #pragma unroll
-    for (int w = 1; w < WR; ++w) M = fmaxf(M, part[w][D]);
+    for (int w = 1; w < WAVES; ++w) M = fmaxf(M, part[w][D]);
     l = 0.f;
     o = f4_t{0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < WR; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float mw = part[w][D], lw = part[w][D + 1];
       if (mw == -INFINITY && lw == 0.f) continue;
       const float al = __builtin_amdgcn_exp2f(mw - M);
@@ -961,7 +962,7 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
     if constexpr (sizeof(T) == 4) gstore_f4(O, o);
     else *reinterpret_cast<uint2 *>(O) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
   }
-  if (a.lse && lane == 0) a.lse[id] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
+  if (a.lse && gl == 0) a.lse[id] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
 }
 
 // ------------------------------------------------------------------------------- launches
@@ -1085,10 +1086,15 @@ hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t
   p.n_few = (int)std::max<int64_t>(1, ceil_div((int64_t)c.few_items * a.heads, WAVES));
   k_runs<D, T><<<p.n_pre + p.n_many + p.n_few, NT, 0, st>>>(p);
   const JoinArgs j{a, pp, pf, pm, entries, c.n_prefix, c.prefix_few, 64 * c.prefix_nq, c.kv_tiles, c.share, c.few_rows, a.n_tok * a.group, c.few_items, c.n_many};
-  // four waves a row where one each would leave most of the chip idle
+  // A workgroup a row, a wave a row or D / 4 lanes a row: as many lanes as fill the chip, since the
+  // chain of reads bounds a row and the lanes that join at its end lengthen it (8192 rows of 10
+  // runs: 11 us by D / 4 lanes, 14 by waves; 2048 rows of 11: 7.3 and 6.0; 384 rows of 171: 9 us by
+  // waves, 6 by workgroups).
   const int64_t out_rows = (int64_t)a.n_tok * a.n_q;
-  if (out_rows < 2 * BLOCKS) k_join<D, T, WAVES><<<(int)out_rows, NT, 0, st>>>(j);
-  else k_join<D, T, 1><<<(int)ceil_div(out_rows, WAVES), NT, 0, st>>>(j);
+  auto grid = [&](int lanes) { return (int)ceil_div(out_rows * lanes, NT); };
+  if (out_rows <= 2 * BLOCKS) k_join<D, T, 64, true><<<grid(NT), NT, 0, st>>>(j);
+  else if (out_rows <= 8 * BLOCKS) k_join<D, T, 64, false><<<grid(64), NT, 0, st>>>(j);
+  else k_join<D, T, D / 4, false><<<grid(D / 4), NT, 0, st>>>(j);
   return hipGetLastError();
 }
 
