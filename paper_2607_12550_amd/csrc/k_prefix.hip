@@ -90,7 +90,8 @@ JOLT_DEV Req request(const PrefixAttendArgs &a, int r) {
 constexpr int FEW_WAVES = 2048, RUN_MIN = 32, RUN_STEP = 32, RUN_PREFIX = 128;
 JOLT_DEV int few_run(int64_t total, int heads) {
   const int64_t c = (total * heads + FEW_WAVES - 1) / FEW_WAVES;
-  return (int)((max(c, (int64_t)RUN_MIN) + RUN_STEP - 1) / RUN_STEP * RUN_STEP);
+  const int64_t in_range = min(max(c, (int64_t)RUN_MIN), (int64_t)1 << 30);   // no tail is longer
+  return (int)((in_range + RUN_STEP - 1) / RUN_STEP * RUN_STEP);
 }
 
 // What the join needs to know of a packed row: its place in its request, whose runs are items

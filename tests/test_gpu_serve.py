@@ -203,20 +203,23 @@ class Batch:
         self.prefix = J.cell_desc(dtype=DT[dtype][0], n_layers=2, n_heads=H, T=T, d=d, stride_layer=H * T * d,
                                   stride_head=T * d, stride_token=d) if T else None
 
-    def run(self, max_new=0, pages=True, prefix=True, stream=None, fill=5.25, ws=None):
+    def run(self, max_new=0, pages=True, prefix=True, stream=None, fill=5.25):
         self.O = torch.full_like(self.Q, fill)
         self.lse = torch.full(self.Q.shape[:2], fill, dtype=torch.float32, device="cuda")
         pre = self.prefix if prefix else None
         pg = self.desc if pages else None
         nb = J.jolt_prefix_attend_workspace_size(len(self.kv_len), self.Q.shape[0], self.Q.shape[1], prefix=pre, pages=pg,
                                                  max_pages=self.table.shape[1] if pages else 0, max_new=max_new)
-        ws = torch.full((nb,), 255, dtype=torch.uint8, device="cuda") if ws is None else ws   # NaN in every type
+        # NaN in every type, and a guard behind the bytes asked for
+        guarded = torch.full((nb + 4096,), 255, dtype=torch.uint8, device="cuda")
+        ws = guarded[:nb]
         note("jolt_prefix_attend", self.dtype, "T", self.T, "rows", self.Q.shape[0], "requests", len(self.kv_len), "H", self.H, "G", self.G,
              "d", self.d, "page", self.page, "max_new", max_new)
         J.jolt_prefix_attend(ctx(), self.Q, self.O, dev_i(self.q_start), dev_i(self.kv_len), self.scale, ws, prefix=pre, K_prefix=self.K,
                              V_prefix=self.V, layer=1 if prefix and self.T else 0, pages=pg, K_pages=self.Kp, V_pages=self.Vp,
                              table=dev_i(self.table), max_new=max_new, lse=self.lse, stream=stream)
         torch.cuda.synchronize()
+        assert (guarded[nb:] == 255).all()
         return f64(self.O), f64(self.lse)
 
     def want(self, pages=True, prefix=True):
@@ -252,6 +255,7 @@ CASES = [  # T, have, new, H, G, d, page
     (513, [0, 200], [40, 70], 2, 3, 64, 16), (260, [9, 0, 0, 50], [1, 130, 0, 7], 2, 8, 32, 128),
     (64, [1, 2, 3], [16, 17, 15], 4, 1, 128, 1024), (0, [700, 0, 5], [1, 33, 2], 1, 16, 64, 32),
     (2050, [300], [1], 1, 64, 128, 16), (33, [4] * 70, [1] * 70, 1, 2, 64, 4),
+    (700, [20, 0, 33], [8, 5, 7], 40, 4, 128, 16), (129, [2, 500], [1, 25], 16, 1, 32, 16),
 ]
 
 
@@ -308,11 +312,11 @@ def test_prefix_attend_layouts_of_pages(layout):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), "lowest"])
-@pytest.mark.parametrize("new", [[1, 1, 1], [3, 2, 3], [40, 2, 37]])
-def test_prefix_attend_ignores_what_a_row_does_not_attend_to(dtype, bad, new):
+@pytest.mark.parametrize("new,d", [([1, 1, 1], 64), ([3, 2, 3], 32), ([7, 5, 8], 128), ([40, 2, 37], 64), ([33, 1, 90], 128)])
+def test_prefix_attend_ignores_what_a_row_does_not_attend_to(dtype, bad, new, d):
     """Whatever stands in unused page slots, behind the lengths and, for the rows before it, in the last token."""
     bad = float(torch.finfo(DT[dtype][1]).min) if bad == "lowest" else bad
-    b = Batch(dtype, 50, [60, 5, 17], new, 2, 4, 64, 16, hole=bad)
+    b = Batch(dtype, 50, [60, 5, 17], new, 2, 4, d, 16, hole=bad)
     want = b.want()
     b.check(b.run(), want)
     # the last token of request 0: keys first, then values; every row but the last is as before
@@ -390,6 +394,47 @@ def test_prefix_attend_equal_calls_give_equal_bits_and_streams_do_not_matter():
     for stream in (None, s, s):
         O2, lse2 = b.run(stream=stream)
         assert (O2 == O).all() and (lse2 == lse).all()
+
+
+def test_prefix_attend_most_requests():
+    rng = np.random.default_rng(0)
+    b = Batch("bf16", 5, rng.integers(0, 40, 4096).tolist(), rng.integers(0, 3, 4096).tolist(), 1, 2, 32, 8)
+    b.check(b.run(max_new=2), b.want())
+
+
+def test_prefix_attend_rows_with_strides():
+    """Q inside the rows of a joint projection, O inside wider rows; nothing beside O's rows is written."""
+    for new in ([1, 1, 0, 2], [30, 1, 2, 40]):
+        b = Batch("bf16", 100, [60, 5, 17, 0], new, 2, 4, 64, 16)
+        want, n = b.want(), b.n_tok
+        wide_q = torch.zeros((n, 8 + 2 * 2, 64), dtype=torch.bfloat16, device="cuda")
+        wide_q[:, 2:10] = b.Q
+        wide_o = torch.full((n, 9, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(J.jolt_prefix_attend_workspace_size(4, n, 8, prefix=b.prefix, pages=b.desc, max_pages=b.table.shape[1]),
+                         dtype=torch.uint8, device="cuda")
+        J.jolt_prefix_attend(ctx(), wide_q[:, 2:10], wide_o[:, :8], dev_i(b.q_start), dev_i(b.kv_len), b.scale, ws, prefix=b.prefix,
+                             K_prefix=b.K, V_prefix=b.V, layer=1, pages=b.desc, K_pages=b.Kp, V_pages=b.Vp, table=dev_i(b.table))
+        torch.cuda.synchronize()
+        O, lse = b.run()
+        assert (f64(wide_o[:, :8]) == O).all() and (wide_o[:, 8] == 7.0).all()
+        b.check((O, lse), want)
+
+
+def test_prefix_attend_calls_at_once():
+    """Calls on several streams, each with a workspace of its own, give what they give alone."""
+    bs = [Batch("bf16", 3000 + 500 * i, [60, 500, 17] * 5, new * 5, 2, 4, 64, 16, seed=i) for i, new in enumerate(([1, 1, 1], [1, 20, 3], [2, 1, 2]))]
+    alone = [b.run() for b in bs]
+    streams = [torch.cuda.Stream() for _ in bs]
+    state = [(torch.empty(J.jolt_prefix_attend_workspace_size(15, b.n_tok, 8, prefix=b.prefix, pages=b.desc, max_pages=b.table.shape[1]),
+                          dtype=torch.uint8, device="cuda"), dev_i(b.q_start), dev_i(b.kv_len), dev_i(b.table), torch.zeros_like(b.Q)) for b in bs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for b, s, (ws, qs, kv, tab, O) in zip(bs, streams, state):
+            J.jolt_prefix_attend(ctx(), b.Q, O, qs, kv, b.scale, ws, prefix=b.prefix, K_prefix=b.K, V_prefix=b.V, layer=1, pages=b.desc,
+                                 K_pages=b.Kp, V_pages=b.Vp, table=tab, stream=s)
+    torch.cuda.synchronize()
+    for (O, _), st in zip(alone, state):
+        assert (f64(st[4]) == O).all()
 
 
 def test_long_tails_past_32_bit_offsets():
