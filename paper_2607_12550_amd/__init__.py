@@ -64,6 +64,7 @@ if not os.path.exists(LIB_PATH):
 import torch  # noqa: E402,F401
 
 lib = C.CDLL(LIB_PATH)
+from . import _marshal  # noqa: E402
 
 
 class CellDesc(C.Structure):
@@ -468,28 +469,6 @@ def page_desc(*, dtype, n_heads, page_size, d, n_pages, stride_page, stride_head
     return PageDesc(dtype, n_heads, page_size, d, n_pages, 0, stride_page, stride_head, stride_token)
 
 
-_TORCH_TYPES = {JOLT_F32: torch.float32, JOLT_BF16: torch.bfloat16}
-_INT32 = torch.int32
-
-
-def _int32s(*checked):
-    """Addresses of contiguous int32 tensors, given as (tensor, elements, name)."""
-    for x, n, name in checked:
-        if x.dtype is not _INT32 or x.numel() != n or not x.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements")
-    return [x.data_ptr() for x, _, _ in checked]
-
-
-def _rows(name, x, n, dtype, n_heads, d):
-    """Token and head strides of an [n, heads, d] tensor whose features are contiguous."""
-    want = _TORCH_TYPES.get(dtype)
-    if x.dtype is not want or x.shape != (n, n_heads, d) or x.stride(2) != 1:
-        raise ValueError(f"{name} must be [{n}, {n_heads}, {d}] of type {want} with contiguous features")
-    # the stride of an axis of one element is never used: it may be anything
-    token, head, _ = x.stride()
-    return RowStrides(token if n > 1 else 0, head if n_heads > 1 else 0)
-
-
 def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, kv_len, q_start, slots, positions,
                    n_free_out, info, stream=None) -> None:
     """Block tables and slot maps of a step from the requests' lengths (device int32 tensors):
@@ -499,25 +478,24 @@ def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, k
     if table.dim() != 2 or table.shape[0] != n:
         raise ValueError("table must be [n_req, max_pages]")
     columns = table.shape[1]
-    h, ad, fr, nf, tb, kv, qs, sl, po, no, inf = _int32s(
-        (have, n, "have"), (add, n, "add"), (free_pages, cap, "free_pages"), (n_free, 1, "n_free"), (table, n * columns, "table"),
-        (kv_len, n, "kv_len"), (q_start, n + 1, "q_start"), (slots, n_tok, "slots"), (positions, n_tok, "positions"),
-        (n_free_out, 1, "n_free_out"), (info, 4, "info"))
+    h, ad, fr, nf, tb, kv, qs, sl, po, no, inf = _marshal.flat(
+        "int32", have, n, "have", add, n, "add", free_pages, cap, "free_pages", n_free, 1, "n_free", table, n * columns, "table",
+        kv_len, n, "kv_len", q_start, n + 1, "q_start", slots, n_tok, "slots", positions, n_tok, "positions",
+        n_free_out, 1, "n_free_out", info, 4, "info")
     _check(lib.jolt_page_plan(ctx, pages, n, h, ad, fr, cap, nf, tb, columns, n_tok, kv, qs, sl, po, no, inf, _stream(stream)))
 
 
 def jolt_page_append(ctx, pages: PageDesc, K, V, slots, K_pages, V_pages, positions=None, rope=None, stream=None) -> None:
     """Writes the rows K, V [n_tok, n_heads, d] into their slots of the pools; rope: None, or
     (base, position_offset) to rotate the keys at positions + position_offset."""
-    n, dtype, heads, d = slots.numel(), pages.dtype, pages.n_heads, pages.d
-    ks, vs = _rows("K", K, n, dtype, heads, d), _rows("V", V, n, dtype, heads, d)
-    if positions is None:
-        (sl,), po = _int32s((slots, n, "slots")), 0
-    else:
-        sl, po = _int32s((slots, n, "slots"), (positions, n, "positions"))
+    n, bf16, heads, d = slots.numel(), pages.dtype == JOLT_BF16, pages.n_heads, pages.d
+    k, _, _, k_token, k_head = _marshal.rows(K, bf16, n, heads, d, "K")
+    v, _, _, v_token, v_head = _marshal.rows(V, bf16, n, heads, d, "V")
+    sl, = _marshal.flat("int32", slots, n, "slots")
+    po = 0 if positions is None else _marshal.flat("int32", positions, n, "positions")[0]
     r = None if rope is None else Rope(float(rope[0]), int(rope[1]), 0)
-    _check(lib.jolt_page_append(ctx, pages, n, sl, po, r, K.data_ptr(), ks, V.data_ptr(), vs, _addr(K_pages), _addr(V_pages),
-                                _stream(stream)))
+    _check(lib.jolt_page_append(ctx, pages, n, sl, po, r, k, RowStrides(k_token, k_head), v, RowStrides(v_token, v_head),
+                                _addr(K_pages), _addr(V_pages), _stream(stream)))
 
 
 def jolt_prefix_attend_workspace_size(n_req: int, n_tok: int, n_q: int, prefix=None, pages=None, max_pages: int = 0,
@@ -541,31 +519,25 @@ def jolt_prefix_attend(ctx, Q, O, q_start, kv_len, scale: float, ws, prefix=None
     desc = pages if pages is not None else prefix
     if desc is None:
         raise ValueError("a prefix or pages are needed")
-    shape, d, want = Q.shape, desc.d, _TORCH_TYPES.get(desc.dtype)
-    if len(shape) != 3 or shape[2] != d or O.shape != shape:
-        raise ValueError(f"Q and O must be [n_tok, n_q, {d}]")
-    n_tok, n_q, _ = shape
-    strides = []
-    for name, x in (("Q", Q), ("O", O)):
-        token, head, one = x.stride()
-        if x.dtype is not want or one != 1 or (head != d and n_q > 1):
-            raise ValueError(f"{name} must be of type {want} with contiguous rows")
-        strides.append(token if n_tok > 1 else n_q * d)
-    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n_tok, n_q) or not lse.is_contiguous()):
-        raise ValueError("lse must be a contiguous fp32 tensor [n_tok, n_q]")
+    d, bf16 = desc.d, desc.dtype == JOLT_BF16
+    q, n_tok, n_q, q_token, q_head = _marshal.rows(Q, bf16, -1, -1, d, "Q")
+    o, _, _, o_token, o_head = _marshal.rows(O, bf16, n_tok, n_q, d, "O")
+    if n_q > 1 and (q_head != d or o_head != d):
+        raise ValueError("the heads of a row of Q and O must be contiguous")
+    ls = 0 if lse is None else _marshal.flat("float32", lse, n_tok * n_q, "lse")[0]
     columns, tab, lens = 0, 0, 0
     if pages is not None:
         if table.dim() != 2 or table.shape[0] != n_req:
             raise ValueError("table must be [n_req, max_pages]")
         columns = table.shape[1]
-        starts, tab, lens = _int32s((q_start, n_req + 1, "q_start"), (table, n_req * columns, "table"), (kv_len, n_req, "kv_len"))
+        starts, tab, lens = _marshal.flat("int32", q_start, n_req + 1, "q_start", table, n_req * columns, "table", kv_len, n_req, "kv_len")
     else:
-        starts, = _int32s((q_start, n_req + 1, "q_start"))
-    b = AttendBatch(n_req, n_tok, n_q, columns, max_new, 0, *strides)
+        starts, = _marshal.flat("int32", q_start, n_req + 1, "q_start")
+    row = n_q * d
+    b = AttendBatch(n_req, n_tok, n_q, columns, max_new, 0, q_token if n_tok > 1 else row, o_token if n_tok > 1 else row)
     wsb = ws_bytes if ws_bytes is not None else (ws.numel() * ws.element_size())
     _check(lib.jolt_prefix_attend(ctx, prefix, _addr(K_prefix), _addr(V_prefix), layer, pages, _addr(K_pages), _addr(V_pages), tab, b,
-                                  starts, lens, Q.data_ptr(), float(scale), O.data_ptr(), _addr(lse), _addr(ws), wsb,
-                                  _stream(stream)))
+                                  starts, lens, q, float(scale), o, ls, _addr(ws), wsb, _stream(stream)))
 
 
 def jolt_debug_export(ctx, what: int, cell: int, dst, stream=None) -> None:

@@ -3,7 +3,8 @@
 Usage: ``python -m paper_2607_12550_amd.build`` (or ``build()`` from Python).
 Every HIP source is compiled for gfx950 only; host-only sources are compiled
 without floating-point contraction so the allocator's double arithmetic is
-plain IEEE.  Objects go to ``_build/`` next to this file.
+plain IEEE.  Objects go to ``_build/`` next to this file.  ``_marshal.so`` is the Python binding's check of
+tensor arguments, against torch's own headers and library.
 """
 from __future__ import annotations
 
@@ -15,6 +16,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libjolt.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 BUILD = os.path.join(HERE, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -40,12 +42,31 @@ def _compile(src: str, extra: list[str]) -> str:
     return obj
 
 
+def _marshal() -> None:
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    inc = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+           sysconfig.get_paths()["include"]]
+    lib = os.path.join(home, "lib")
+    cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *[f"-isystem{d}" for d in inc], os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL + ".tmp", f"-L{lib}",
+           "-ltorch_python", "-ltorch_cpu", "-lc10", f"-Wl,-rpath,{lib}"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("building _marshal.so failed:\n" + r.stdout + r.stderr)
+    os.replace(MARSHAL + ".tmp", MARSHAL)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     jobs = [(s, DEVICE_FLAGS) for s in DEVICE_SOURCES] + [(s, []) for s in HOST_SOURCES] + \
            [(s, ["-ffp-contract=off"]) for s in STRICT_FP_SOURCES]
     with ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
+        marshal = ex.submit(_marshal)
         objs = list(ex.map(lambda j: _compile(*j), jobs))
+        marshal.result()
     tmp = OUT + ".tmp"
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -462,6 +462,39 @@ def test_long_tails_past_32_bit_offsets():
     assert int((pool != 0).any(-1).sum()) == H * (page + 1)
 
 
+def test_tensor_arguments_are_checked_before_the_library():
+    """Types, sizes and layouts that do not fit are refused by the binding (the null context would
+    end every call before device work)."""
+    A = 1 << 20
+    pages = J.page_desc(dtype=J.JOLT_BF16, n_heads=8, page_size=16, d=128, n_pages=100, stride_page=8 * 16 * 128,
+                        stride_head=16 * 128, stride_token=128)
+    z = torch.zeros(4, dtype=torch.int32, device="cuda")
+    t = torch.zeros((4, 3), dtype=torch.int32, device="cuda")
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = dict(have=z, add=z, free_pages=z, n_free=one, table=t, kv_len=z.clone(), q_start=torch.zeros(5, dtype=torch.int32, device="cuda"),
+                slots=z.clone(), positions=z.clone(), n_free_out=one.clone(), info=z.clone())
+    bad = dict(have=z.long(), add=z[:3], n_free=z, table=t[:2], kv_len=t[:, 0], q_start=z, positions=z[:2], n_free_out=z, info=one)
+    for k, v in bad.items():
+        with pytest.raises(ValueError):
+            J.jolt_page_plan(None, pages, **{**args, k: v})
+    K = torch.zeros((4, 8, 128), dtype=torch.bfloat16, device="cuda")
+    for k, v in ((K.float(), K), (K, K[:, :4]), (K[:3], K), (K.transpose(1, 2), K), (K, K[..., ::2])):
+        with pytest.raises(ValueError):
+            J.jolt_page_append(None, pages, k, v, z, A, 2 * A)
+    Q = torch.zeros((4, 32, 128), dtype=torch.bfloat16, device="cuda")
+    qs = torch.zeros(5, dtype=torch.int32, device="cuda")
+    for kw in (dict(Q=Q.float()), dict(O=Q[:3]), dict(lse=torch.zeros(4, 32, dtype=torch.float64, device="cuda")), dict(kv_len=z[:2]),
+               dict(table=t[:2]), dict(q_start=qs[:3]), dict(Q=Q.transpose(0, 1)), dict(pages=None), dict(Q=Q.cpu())):
+        a = dict(Q=Q, O=Q.clone(), q_start=qs, kv_len=z, scale=0.1, ws=A, pages=pages, K_pages=A, V_pages=A, table=t, ws_bytes=1)
+        with pytest.raises(ValueError):
+            J.jolt_prefix_attend(None, **{**a, **kw})
+    ok = dict(Q=Q, O=Q.clone(), q_start=qs, kv_len=z, scale=0.1, ws=A, pages=pages, K_pages=A, V_pages=2 * A, table=t, ws_bytes=1 << 40)
+    for call in (lambda: J.jolt_page_plan(None, pages, **args), lambda: J.jolt_page_append(None, pages, K, K, z, A, 2 * A),
+                 lambda: J.jolt_prefix_attend(None, **ok)):
+        with pytest.raises(J.JoltError, match="ctx is null"):
+            call()
+
+
 # ------------------------------------------------------------------------------- a step
 class Server:
     """The three operators as a serving loop uses them, with the oracle's state beside them."""

@@ -142,28 +142,21 @@ def test_prefix_attend_refuses_bad_arguments():
     _refused(_attend(nb=need), J.JOLT_E_INVAL, "ctx is null")
 
 
-def test_tensor_arguments_are_checked_before_the_library():
+def test_tensors_off_the_gpu_are_refused():
+    """The binding takes GPU tensors only; a host tensor never reaches a kernel."""
     import torch
-    z = torch.zeros(4, dtype=torch.int32)
+    z = [torch.zeros(n, dtype=torch.int32) for n in (4, 4, 4, 1, 4, 5, 4, 4, 1, 4)]
     t = torch.zeros((4, 3), dtype=torch.int32)
-    one = torch.zeros(1, dtype=torch.int32)
-    args = dict(have=z, add=z, free_pages=z, n_free=one, table=t, kv_len=z.clone(), q_start=torch.zeros(5, dtype=torch.int32),
-                slots=z.clone(), positions=z.clone(), n_free_out=one.clone(), info=z.clone())
-    bad = dict(have=z.long(), add=z[:3], n_free=z, table=t[:2], kv_len=t[:, 0], q_start=z, positions=z[:2], n_free_out=z, info=one)
-    for k, v in bad.items():
-        with pytest.raises(ValueError):
-            J.jolt_page_plan(None, _pages(), **{**args, k: v})
+    with pytest.raises(ValueError, match="on the GPU"):
+        J.jolt_page_plan(None, _pages(), *z[:4], t, *z[4:])
     K = torch.zeros((4, 8, 128), dtype=torch.bfloat16)
-    for k, v in ((K.float(), K), (K, K[:, :4]), (K[:3], K), (K.transpose(1, 2), K), (K, K[..., ::2])):
-        with pytest.raises(ValueError):
-            J.jolt_page_append(None, _pages(), k, v, z, A, 2 * A)
+    with pytest.raises(ValueError, match="on the GPU"):
+        J.jolt_page_append(None, _pages(), K, K, z[0], A, 2 * A)
     Q = torch.zeros((4, 32, 128), dtype=torch.bfloat16)
-    qs = torch.zeros(5, dtype=torch.int32)
-    for kw in (dict(Q=Q.float()), dict(O=Q[:3]), dict(lse=torch.zeros(4, 32, dtype=torch.float64)), dict(kv_len=z[:2]),
-               dict(table=t[:2]), dict(q_start=qs[:3]), dict(Q=Q.transpose(0, 1)), dict(pages=None)):
-        a = dict(Q=Q, O=Q.clone(), q_start=qs, kv_len=z, scale=0.1, ws=A, pages=_pages(), K_pages=A, V_pages=A, table=t, ws_bytes=1)
-        with pytest.raises(ValueError):
-            J.jolt_prefix_attend(None, **{**a, **kw})
+    with pytest.raises(ValueError, match="on the GPU"):
+        J.jolt_prefix_attend(None, Q, Q, z[5], z[0], 0.1, A, pages=_pages(), K_pages=A, V_pages=A, table=t, ws_bytes=1)
+    with pytest.raises(ValueError, match="must be a tensor"):
+        J.jolt_page_append(None, _pages(), [1], K, z[0], A, 2 * A)
 
 
 # ------------------------------------------------------------------------------ the oracle
