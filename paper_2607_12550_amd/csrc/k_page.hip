@@ -16,9 +16,10 @@ constexpr int NT = 256, WAVES = NT / 64;
 // for itself, which takes one launch instead of a scan and a second kernel that waits for it.
 // Workgroup 0 writes the per-request outputs.
 //
-// A thread takes four rows in a row: one bisection for the first, the others step on from it, and
-// their page reads are under way together.
-constexpr int PLAN_STEP = 4, PLAN_ROWS = PLAN_STEP * NT;   // packed rows of a thread, of a workgroup
+// A thread takes STEP rows in a row: one bisection for the first, the others step on from it, and
+// their page reads are under way together.  Four where one each would take more workgroups than
+// the chip has CUs to repeat the sums (131,000 rows of 500 requests: 6.2 us, 7.8 by one each); one
+// where rows are few (64 rows: 3.5 us, 4.7 by four).
 
 JOLT_DEV int64_t wave_scan(int64_t v, int lane) {   // inclusive
 #pragma unroll
@@ -29,6 +30,7 @@ JOLT_DEV int64_t wave_scan(int64_t v, int lane) {   // inclusive
   return v;
 }
 
+template <int STEP>
 __global__ void __launch_bounds__(NT) k_page_plan(const PagePlanArgs a) {
   extern __shared__ int32_t lds[];
   int32_t *start = lds;                    // [n_req + 1] first packed row
@@ -91,9 +93,9 @@ __global__ void __launch_bounds__(NT) k_page_plan(const PagePlanArgs a) {
   }
   if (!why && tid == 0) start[a.n_req] = (int)all_rows;
   __syncthreads();
-  const int t0 = (blockIdx.x * NT + tid) * PLAN_STEP;
+  const int t0 = (blockIdx.x * NT + tid) * STEP;
   if (t0 >= a.n_tok) return;
-  int slot[PLAN_STEP], pos[PLAN_STEP], req[PLAN_STEP], page[PLAN_STEP];
+  int slot[STEP], pos[STEP], req[STEP], page[STEP];
   int lo = 0;
   if (!why && t0 < all_rows) {
     int hi = a.n_req;                      // start[lo] <= t0 < start[hi]
@@ -103,7 +105,7 @@ __global__ void __launch_bounds__(NT) k_page_plan(const PagePlanArgs a) {
     }
   }
 #pragma unroll
-  for (int i = 0; i < PLAN_STEP; ++i) {
+  for (int i = 0; i < STEP; ++i) {
     const int t = t0 + i;
     slot[i] = pos[i] = -1;
     req[i] = -1;
@@ -116,13 +118,13 @@ __global__ void __launch_bounds__(NT) k_page_plan(const PagePlanArgs a) {
     page[i] = fresh >= 0 ? a.free_pages[n_free - 1 - (first[lo] + fresh)] : a.table[(int64_t)lo * a.max_pages + j];
   }
 #pragma unroll
-  for (int i = 0; i < PLAN_STEP; ++i)
+  for (int i = 0; i < STEP; ++i)
     if (req[i] >= 0) {
       if ((pos[i] & mask) == 0) a.table[(int64_t)req[i] * a.max_pages + (pos[i] >> sh)] = page[i];
       if ((uint32_t)page[i] < (uint32_t)a.n_pages) slot[i] = (page[i] << sh) + (pos[i] & mask);
     }
 #pragma unroll
-  for (int i = 0; i < PLAN_STEP; ++i)
+  for (int i = 0; i < STEP; ++i)
     if (t0 + i < a.n_tok) {
       a.slots[t0 + i] = slot[i];
       a.positions[t0 + i] = pos[i];
@@ -209,8 +211,10 @@ hipError_t append(const PageAppendArgs &a, int dtype, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_page_plan(const PagePlanArgs &a, hipStream_t st) {
-  const int grid = (a.n_tok + PLAN_ROWS - 1) / PLAN_ROWS;
-  k_page_plan<<<grid, NT, (3 * a.n_req + 1) * sizeof(int32_t), st>>>(a);
+  const size_t lds = (3 * a.n_req + 1) * sizeof(int32_t);
+  auto grid = [&](int step) { return (a.n_tok + step * NT - 1) / (step * NT); };
+  if (a.n_tok <= 256 * NT) k_page_plan<1><<<grid(1), NT, lds, st>>>(a);
+  else k_page_plan<4><<<grid(4), NT, lds, st>>>(a);
   return hipGetLastError();
 }
 
