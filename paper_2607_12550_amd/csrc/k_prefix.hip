@@ -86,7 +86,11 @@ JOLT_DEV Req request(const PrefixAttendArgs &a, int r) {
 
 // Runs of the requests that few() serves: of equal length (a multiple of a wave's step), about
 // FEW_WAVES runs of a head over all heads besides one a request, in the requests' order.  Every
-// workgroup forms the sums for itself, from one read of the lengths.
+// workgroup forms the sums for itself, from one read of the lengths.  2048 waves, two a SIMD, and
+// runs down to one step: with 512, 1024, 2048 and 4096 waves the tails of 256 requests of 148
+// tokens take 82, 60, 56 and 54 us, 12 of 1700 tokens 34, 35, 31 and 38; with runs of at least 128
+// tokens 32 fp32 requests of 45 take 22 us a call, 14 with runs of 32.  A run of the prefix is
+// four waves' (RUN_PREFIX): of 512 tokens instead, 4096 tokens under 16 rows take 16 us, not 12.
 constexpr int FEW_WAVES = 2048, RUN_MIN = 32, RUN_STEP = 32, RUN_PREFIX = 128;
 JOLT_DEV int few_run(int64_t total, int heads) {
   const int64_t c = (total * heads + FEW_WAVES - 1) / FEW_WAVES;
@@ -967,16 +971,6 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
 }
 
 // ------------------------------------------------------------------------------- launches
-// How a call is cut, from its sizes alone (the workspace depends on it too).
-struct Cut {
-  bool prefix_few = false, tails_many = false;
-  int prefix_nq = 1, prefix_run = 0, n_prefix = 0;
-  int prefix_tiles = 0, prefix_groups = 0, kv_tiles = 0;     // of many()
-  int64_t share = 1;
-  int few_nq = 1, few_items = 0, few_rows = 0, limit = 0;
-  int many_nq = 1, many_tiles = 0, n_many = 0;
-  size_t off_po, off_pm, off_fo, off_fm, off_mo, off_mm, off_entries, total;
-};
 constexpr int BLOCKS = 512;        // workgroups that fill the chip: two a CU
 
 int64_t ceil_div(int64_t x, int64_t y) { return (x + y - 1) / y; }
@@ -985,19 +979,23 @@ int64_t ceil_div(int64_t x, int64_t y) { return (x + y - 1) / y; }
 // workgroup that has its CU to itself takes about `tile` us a tile of keys and values (the matrix
 // work, and a part that waits for memory and LDS) and 4 us to start and end a row tile; two on a
 // CU take 1.5 times as long as one; every run's output is written and read once more, at about
-// 4 MB a us and 0.1 us a run of a row.
-void cut_prefix(Cut &c, const PrefixAttendArgs &a, int d, bool bf16) {
+// 4 MB a us and 0.1 us a run of a row.  Measured against it (prefix alone, us): 256 rows a head on
+// 4096 tokens, 64-row tiles in 4, 8, 16 and 32 runs 32, 22, 22 and 27, 128-row tiles 41, 27, 23 and
+// 25; 1024 rows on 32768 tokens, 8 runs 251 and 192.
+void cut_prefix(PrefixCut &c, const PrefixAttendArgs &a, int d, bool bf16) {
   const int64_t rows = (int64_t)a.n_tok * a.group, tokens = bf16 ? 64 : 32;
   const double out = (double)a.n_tok * a.n_q * d * 8 / 4e6;
+  const int most = std::max(1, BLOCKS / a.heads);      // workgroups of a head
   double best = 0;
   c.n_prefix = 0;
   c.kv_tiles = (int)ceil_div(a.T, tokens);
   for (int nq = 1; nq <= 2; ++nq) {
     const int64_t tiles = ceil_div(rows, 64 * nq), pairs = tiles * c.kv_tiles;
     const double tile = 0.3 + (bf16 ? 0.9 : 3.4) * d / 128 * nq / 2;
-    for (int64_t of = std::max<int64_t>(1, BLOCKS / a.heads); of >= 1; of = of * 7 / 8) {   // workgroups of a head
+    // past a sixteenth of the chip only a call with nothing to share out is left
+    for (int of = most; of >= std::max(1, most / 16); of = of * 3 / 4) {
       const int64_t share = ceil_div(pairs, of), n = a.heads * ceil_div(pairs, share);
-      const double slabs = (double)share >= c.kv_tiles ? 1 + (double)(c.kv_tiles - 1) / share : (double)c.kv_tiles / share;
+      const double slabs = share >= c.kv_tiles ? 1 + (double)(c.kv_tiles - 1) / share : (double)c.kv_tiles / share;
       const double rounds = 1.5 * (n / BLOCKS) + (n % BLOCKS == 0 ? 0 : n % BLOCKS <= BLOCKS / 2 ? 1 : 1.5);
       const double cost = rounds * (tile * share + 4 * (1 + (double)(share - 1) / c.kv_tiles)) + slabs * (out + 0.1);
       if (c.n_prefix == 0 || cost < best) {
@@ -1012,56 +1010,8 @@ void cut_prefix(Cut &c, const PrefixAttendArgs &a, int d, bool bf16) {
   }
 }
 
-Cut cut(const PrefixAttendArgs &a, int d, bool bf16) {
-  Cut c;
-  const int64_t rows = (int64_t)a.n_tok * a.group;     // rows of a key-value head
-  if (a.T > 0) {
-    c.prefix_few = rows <= 32;
-    if (c.prefix_few) {
-      c.prefix_nq = rows <= 16 ? 1 : 2;
-      const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(ceil_div(a.T, RUN_PREFIX), BLOCKS / a.heads));
-      c.prefix_run = (int)(ceil_div(ceil_div(a.T, runs), RUN_PREFIX) * RUN_PREFIX);
-      c.n_prefix = (int)ceil_div(a.T, c.prefix_run);
-    } else {
-      cut_prefix(c, a, d, bf16);
-    }
-  }
-  // without tails every request is one of few rows and no runs
-  c.limit = 0x7fffffff;
-  if (a.max_pages > 0) {
-    const int64_t most = (int64_t)a.max_new * a.group; // rows of a request
-    c.few_nq = most <= 16 ? 1 : 2;
-    c.limit = 16 * c.few_nq;
-    c.few_rows = (int)std::min<int64_t>(most, c.limit);
-    c.few_items = FEW_WAVES / a.heads + a.n_req;
-    c.tails_many = most > c.limit;
-    if (c.tails_many) {
-      c.many_nq = most <= 64 ? 1 : 2;
-      // a request of more than `limit` rows has at most one tile that is not full
-      c.many_tiles = (int)(rows / (64 * c.many_nq) + std::min<int64_t>(a.n_req, rows / (c.limit + 1)));
-      const int64_t want = BLOCKS / ((int64_t)a.heads * c.many_tiles);
-      c.n_many = (int)std::max<int64_t>(1, std::min<int64_t>(want, 16));
-    }
-  }
-  size_t off = 0;
-  auto take = [&](size_t n) {
-    const size_t at = off;
-    off += (n + 255) / 256 * 256;
-    return at;
-  };
-  const size_t np = c.prefix_few ? (size_t)c.n_prefix * a.heads * rows : (size_t)c.n_prefix * a.n_tok * a.n_q;
-  const size_t nf = (size_t)c.few_items * a.heads * c.few_rows;
-  const size_t nm = (size_t)c.n_many * a.n_tok * a.n_q;
-  c.off_po = take(np * d * 4); c.off_pm = take(np * 8);
-  c.off_fo = take(nf * d * 4); c.off_fm = take(nf * 8);
-  c.off_mo = take(nm * d * 4); c.off_mm = take(nm * 8);
-  c.off_entries = take((size_t)a.n_tok * sizeof(RowEntry));
-  c.total = off;
-  return c;
-}
-
 template <int D, class T>
-hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t st) {
+hipError_t run(const PrefixAttendArgs &a, const PrefixCut &c, uint8_t *ws, hipStream_t st) {
   auto parts = [&](size_t o, size_t m) { return Parts{reinterpret_cast<float *>(ws + o), reinterpret_cast<float2 *>(ws + m)}; };
   const Parts pp = parts(c.off_po, c.off_pm), pf = parts(c.off_fo, c.off_fm), pm = parts(c.off_mo, c.off_mm);
   RowEntry *entries = reinterpret_cast<RowEntry *>(ws + c.off_entries);
@@ -1101,10 +1051,57 @@ hipError_t run(const PrefixAttendArgs &a, const Cut &c, uint8_t *ws, hipStream_t
 
 }  // namespace
 
-size_t prefix_attend_workspace(const PrefixAttendArgs &a, int d, int dtype) { return cut(a, d, dtype == JOLT_BF16).total; }
+PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype) {
+  PrefixCut c;
+  const int64_t rows = (int64_t)a.n_tok * a.group;     // rows of a key-value head
+  if (a.T > 0) {
+    // Up to 32 rows few() reads the prefix at the rate of memory: 32 rows on 32768 tokens of 8 heads
+    // take 38 us, 44 by many(); 17 rows on 4001 tokens of 40 heads 29 and 32.
+    c.prefix_few = rows <= 32;
+    if (c.prefix_few) {
+      c.prefix_nq = rows <= 16 ? 1 : 2;
+      const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(ceil_div(a.T, RUN_PREFIX), BLOCKS / a.heads));
+      c.prefix_run = (int)(ceil_div(ceil_div(a.T, runs), RUN_PREFIX) * RUN_PREFIX);
+      c.n_prefix = (int)ceil_div(a.T, c.prefix_run);
+    } else {
+      cut_prefix(c, a, d, dtype == JOLT_BF16);
+    }
+  }
+  // without tails every request is one of few rows and no runs
+  c.limit = 0x7fffffff;
+  if (a.max_pages > 0) {
+    // Requests of up to 32 rows by few(), also where that takes two groups of rows a wave: 64 requests
+    // of up to 32 rows and 500 tokens take 22 us, 26 with those past 16 rows by many() (fp32 33, 64).
+    const int64_t most = (int64_t)a.max_new * a.group; // rows of a request
+    c.few_nq = most <= 16 ? 1 : 2;
+    c.limit = 16 * c.few_nq;
+    c.few_rows = (int)std::min<int64_t>(most, c.limit);
+    c.few_items = FEW_WAVES / a.heads + a.n_req;
+    c.tails_many = most > c.limit;
+    if (c.tails_many) {
+      c.many_nq = most <= 64 ? 1 : 2;
+      // a request of more than `limit` rows has at most one tile that is not full
+      c.many_tiles = (int)(rows / (64 * c.many_nq) + std::min<int64_t>(a.n_req, rows / (c.limit + 1)));
+      const int64_t want = BLOCKS / ((int64_t)a.heads * c.many_tiles);
+      c.n_many = (int)std::max<int64_t>(1, std::min<int64_t>(want, 16));
+    }
+  }
+  auto take = [&](size_t n) {
+    const size_t at = c.ws_bytes;
+    c.ws_bytes += (n + 255) / 256 * 256;
+    return at;
+  };
+  const size_t np = c.prefix_few ? (size_t)c.n_prefix * a.heads * rows : (size_t)c.n_prefix * a.n_tok * a.n_q;
+  const size_t nf = (size_t)c.few_items * a.heads * c.few_rows;
+  const size_t nm = (size_t)c.n_many * a.n_tok * a.n_q;
+  c.off_po = take(np * d * 4); c.off_pm = take(np * 8);
+  c.off_fo = take(nf * d * 4); c.off_fm = take(nf * 8);
+  c.off_mo = take(nm * d * 4); c.off_mm = take(nm * 8);
+  c.off_entries = take((size_t)a.n_tok * sizeof(RowEntry));
+  return c;
+}
 
-hipError_t launch_prefix_attend(const PrefixAttendArgs &a, int d, int dtype, void *ws, hipStream_t st) {
-  const Cut c = cut(a, d, dtype == JOLT_BF16);
+hipError_t launch_prefix_attend(const PrefixAttendArgs &a, const PrefixCut &c, int d, int dtype, void *ws, hipStream_t st) {
   uint8_t *w = static_cast<uint8_t *>(ws);
   if (dtype == JOLT_BF16)
     return d == 32 ? run<32, bf16_t>(a, c, w, st) : d == 64 ? run<64, bf16_t>(a, c, w, st) : run<128, bf16_t>(a, c, w, st);

@@ -272,8 +272,18 @@ struct PrefixAttendArgs {
   int32_t T, max_pages, max_new;               // T = 0: no prefix
   float scale;
 };
-size_t prefix_attend_workspace(const PrefixAttendArgs &a, int d, int dtype);
-hipError_t launch_prefix_attend(const PrefixAttendArgs &a, int d, int dtype, void *ws, hipStream_t st);
+// How a call is cut into runs, from its sizes alone, and where its workspace keeps their results.
+struct PrefixCut {
+  bool prefix_few = false, tails_many = false;
+  int32_t prefix_nq = 1, prefix_run = 0, n_prefix = 0;           // few(): tokens of a run; runs of a row
+  int32_t prefix_tiles = 0, prefix_groups = 0, kv_tiles = 0;     // many(): row tiles, workgroups of a head
+  int64_t share = 1;                                             // and (row tile, tile of tokens) pairs of each
+  int32_t few_nq = 1, few_items = 0, few_rows = 0, limit = 0;    // tails of few rows
+  int32_t many_nq = 1, many_tiles = 0, n_many = 0;               // and of many
+  size_t off_po = 0, off_pm = 0, off_fo = 0, off_fm = 0, off_mo = 0, off_mm = 0, off_entries = 0, ws_bytes = 0;
+};
+PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype);
+hipError_t launch_prefix_attend(const PrefixAttendArgs &a, const PrefixCut &c, int d, int dtype, void *ws, hipStream_t st);
 
 // ----------------------------------------------------------------- eigensolver
 struct EigBatch {

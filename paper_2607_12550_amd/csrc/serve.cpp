@@ -181,7 +181,7 @@ extern "C" int jolt_prefix_attend_workspace_size(const jolt_cell_desc *prefix, c
   int rc = resolve_prefix_attend(prefix, pages, batch, &a, &d, &dtype);
   if (rc) return rc;
   if (!bytes) return jolt_fail(JOLT_E_INVAL, "bytes is null");
-  *bytes = prefix_attend_workspace(a, d, dtype);
+  *bytes = prefix_attend_cut(a, d, dtype).ws_bytes;
   return JOLT_OK;
 }
 
@@ -205,8 +205,8 @@ extern "C" int jolt_prefix_attend(jolt_ctx *ctx, const jolt_cell_desc *prefix, c
     return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: Q, O, keys and values must be 16-byte aligned");
   if (misaligned(ws, 256)) return jolt_fail(JOLT_E_INVAL, "workspace must be 256-byte aligned");
   if (!(scale > 0.f) || !std::isfinite(scale)) return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: scale must be > 0");
-  const size_t need = prefix_attend_workspace(a, d, dtype);
-  if (ws_bytes < need) return jolt_fail(JOLT_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+  const PrefixCut cut = prefix_attend_cut(a, d, dtype);
+  if (ws_bytes < cut.ws_bytes) return jolt_fail(JOLT_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, cut.ws_bytes);
   if (!ctx) return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: ctx is null");
   DeviceGuard dg;
   HIP_OK(dg.enter(ctx->device));
@@ -225,6 +225,6 @@ extern "C" int jolt_prefix_attend(jolt_ctx *ctx, const jolt_cell_desc *prefix, c
   }
   a.q_start = q_start; a.Q = Q; a.O = O; a.lse = lse; a.scale = scale;
   StageTimer t(ctx, st, JOLT_STAGE_PREFIX_ATTEND);
-  HIP_OK(launch_prefix_attend(a, d, dtype, ws, st));
+  HIP_OK(launch_prefix_attend(a, cut, d, dtype, ws, st));
   return JOLT_OK;
 }
