@@ -15,6 +15,8 @@
  *                     stored factors, randomized Hadamard rotation and b-bit
  *                     group quantisation (section 4 "Rotated residual").
  *   jolt_decompress : X^ = X~ + rotation^-1(dequantised residual).
+ *   jolt_page_plan, jolt_page_append, jolt_prefix_attend : a batch of requests that goes on
+ *                     from one shared prefix, each with its own pages.
  *
  * Conventions shared by every entry point:
  *   - Return JOLT_OK (0) or a negative JOLT_E_* code; jolt_last_error() gives a
@@ -498,7 +500,7 @@ typedef struct {
  * values summed in fp32, scores and softmax in fp32, the softmax weights rounded to bf16 for
  * the value product, O rounded once.  fp32: fp32 throughout.  Results do not depend on the
  * order of arrival of anything (no atomics): equal calls give equal bits.
- * O and lse overlap no input.  ws: device, 256-byte aligned, at least
+ * O and lse overlap no input.  At most 1024 key-value heads, n_tok * n_q < 2^28.  ws: device, 256-byte aligned, at least
  * jolt_prefix_attend_workspace_size bytes, not shared by calls that may run at the same time.
  * Errors: JOLT_E_INVAL, JOLT_E_UNSUPPORTED, JOLT_E_WORKSPACE. */
 int jolt_prefix_attend_workspace_size(const jolt_cell_desc *prefix, const jolt_page_desc *pages,

@@ -3,8 +3,8 @@
 // A query head's rows of one key-value head h are numbered rho = (token) * G + (head in its
 // group), so that all rows that read head h stand side by side: those of the whole batch for
 // the prefix, those of one request for its tail.  Both parts are cut into runs of tokens, each
-// run keeps the running maximum m (in units of log2) and sum l of its softmax and the sum of
-// exp2(s - m) v, and the last kernel joins the runs of a row.
+// run keeps a reference m near the largest score (in units of log2), the sum l of exp2(s - m) and
+// the sum of exp2(s - m) v, and the last kernel joins the runs of a row.
 //
 //  * few:  at most 16 NQ rows.  Reading the keys and values bounds it, so the four waves of a
 //    workgroup take different tokens of the run, keys go from memory straight into the matrix
@@ -261,10 +261,13 @@ struct Rows {
     if (__builtin_expect(__any(far), 0)) {
 #pragma unroll
       for (int x = 0; x < NQ; ++x) {
+        // only where this query's own lanes say so: no row's rounding depends on another's values
+        const bool mine = !(sum[x] <= 65536.f) || m[x] == -INFINITY;
         float mx = max4(s[0][x]);
 #pragma unroll
         for (int u = 1; u < SUBS; ++u) mx = fmaxf(mx, max4(s[u][x]));
         mx = fmaxf(m[x], over_groups_max(mx) * c);
+        if (over_groups_max(mine ? 1.f : 0.f) == 0.f) mx = m[x];
         // nothing seen so far: both are -inf, and nothing is there to rescale
         const float al = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[x] - mx);
         l[x] *= al;

@@ -360,6 +360,20 @@ def test_prefix_attend_leaves_rows_behind_the_last_request():
         b.check(b.run(), b.want())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prefix_attend_rows_do_not_depend_on_their_neighbours(dtype):
+    """What stands in rows of no request, and in the other rows, does not move a bit of a row."""
+    for new in ([1, 0, 1], [30, 2, 0], [60, 5, 33]):
+        b = Batch(dtype, 300, [60, 5, 17], new, 2, 4, 64, 16, pad_rows=37)
+        n, n0 = int(b.q_start[-1]), int(b.q_start[1])
+        first = b.run()
+        for fill in (float("nan"), 1e4, -float("inf")):
+            b.Q[n:] = fill
+            b.Q[n0:n] = 30 * torch.randn_like(b.Q[n0:n])
+            O, lse = b.run()
+            assert (O[:n0] == first[0][:n0]).all() and (lse[:n0] == first[1][:n0]).all()
+
+
 def test_prefix_attend_bounds_lengths_and_pages_that_are_wrong():
     """Lengths past the table, pages outside the pool, starts past the rows: nothing outside is
     read or written (checked on the rows that are still well defined)."""
