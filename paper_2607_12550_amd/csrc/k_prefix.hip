@@ -12,7 +12,8 @@
 //  * many: 64 NQ rows a workgroup, which share the tiles of keys and values in LDS: the
 //    prefix is read once per row tile instead of once per request, and the matrix cores bound it.
 //  * k_join: the runs of a row.
-// k_runs holds few and many, for the prefix and for the tails, in one launch.
+// k_runs holds few and many, for the prefix and for the tails, in one launch.  A short call is one
+// launch altogether: k_whole is few on a request's prefix and tail, and ends with its output.
 //
 // Products are formed transposed, S^T = K Q^T and O^T = V^T P^T: the matrix instruction then
 // leaves the scores of 4 neighbouring tokens of one query in a lane, which are the weights that
@@ -416,17 +417,32 @@ struct FewLds {
   FindLds<WAVES> f;
 };
 
-template <int D, class T, int NQ, bool TAIL>
+// Features e .. e + 3 of row t, query head j, from the joined sum o, reference M and sum l.
+template <int D, class T>
+JOLT_DEV void write_row(const PrefixAttendArgs &a, int t, int j, int e, f4_t o, float M, float l, bool first) {
+  T *O = static_cast<T *>(a.O) + (int64_t)t * a.o_stride + (int64_t)j * D + e;
+  o *= l == 0.f ? 0.f : 1.f / l;
+  if constexpr (sizeof(T) == 4) gstore_f4(O, o);
+  else *reinterpret_cast<uint2 *>(O) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+  if (a.lse && first) a.lse[(int64_t)t * a.n_q + j] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
+}
+
+// What few() takes: runs of the prefix, runs of the tails, or requests as a whole, the prefix and
+// then the tail, with their output.
+enum { FEW_PREFIX = 0, FEW_TAIL, FEW_WHOLE };
+
+template <int D, class T, int NQ, int MODE>
 JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds<D, T, NQ> &sm) {
   using G = Geo<D, T>;
-  const PrefixSource &src = TAIL ? a.tail : a.prefix;
+  constexpr bool TAIL = MODE != FEW_PREFIX, OWN = MODE == FEW_TAIL, WHOLE = MODE == FEW_WHOLE;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, g = lane >> 4;
-  const int id = TAIL ? block * WAVES + wave : block;      // item * heads + h
+  const int id = OWN ? block * WAVES + wave : block;       // item (WHOLE: request) * heads + h
   const int h = id % a.heads, item = id / a.heads;
-  constexpr int STRIDE = TAIL ? G::TPW : WAVES * G::TPW;   // tokens from a wave's step to its next
+  constexpr int STRIDE = OWN ? G::TPW : WAVES * G::TPW;    // tokens from a wave's step to its next
   int t0, n, first, end, len = 0;
+  int tail0 = 0;                     // the tail's token 0 in the run's count: WHOLE, after the prefix's last step
   const int32_t *pages = nullptr;
-  if constexpr (TAIL) {
+  if constexpr (OWN) {
     int want[WAVES];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) want[w] = (block * WAVES + w) / a.heads;
@@ -439,6 +455,16 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
     first = f.idx * f.run;
     end = min(len, first + f.run);
     pages = a.table + (int64_t)f.r * a.max_pages;
+  } else if constexpr (WHOLE) {
+    const Req x = request(a, item);
+    if (x.n == 0) return;
+    t0 = x.q0;
+    n = x.n;
+    len = x.len;
+    first = 0;
+    tail0 = (a.T + G::TPW - 1) / G::TPW * G::TPW;
+    end = tail0 + len;
+    pages = a.table + (int64_t)item * a.max_pages;
   } else {
     t0 = 0;
     n = a.n_tok;
@@ -460,20 +486,27 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
   }
   const float c = a.scale * LOG2E;
   uint8_t *vl = sm.w[wave];
-  const uint8_t *Kb = static_cast<const uint8_t *>(src.K), *Vb = static_cast<const uint8_t *>(src.V);
   ju4 kr[G::SUB][G::KS], vr[G::SUB][G::KS];
   RowAt at[G::SUB];
   int pg[G::SUB];
-  const int x0 = first + (TAIL ? 0 : wave * G::TPW);
+  const int x0 = first + (OWN ? 0 : wave * G::TPW);
+  // whether the step at x is of the tail; it is of one part as a whole
+  auto of_tail = [&](int x) { return OWN || (WHOLE && x >= tail0); };
   auto ask_pages = [&](int x) {
+    if (of_tail(x))
 #pragma unroll
-    for (int u = 0; u < G::SUB; ++u) pg[u] = page_of(src, pages, x + 16 * u + n16, end);
+      for (int u = 0; u < G::SUB; ++u) pg[u] = page_of(a.tail, pages, x - tail0 + 16 * u + n16, OWN ? end : len);
   };
   auto place = [&](int x) {
+    const bool tail = of_tail(x);
 #pragma unroll
-    for (int u = 0; u < G::SUB; ++u) at[u] = row_at(src, pg[u], h, x + 16 * u + n16, end, sizeof(T));
+    for (int u = 0; u < G::SUB; ++u)
+      at[u] = tail ? row_at(a.tail, pg[u], h, x - tail0 + 16 * u + n16, OWN ? end : len, sizeof(T))
+                   : row_at(a.prefix, 0, h, x + 16 * u + n16, WHOLE ? a.T : end, sizeof(T));
   };
-  auto load = [&](const uint8_t *base, ju4 (&d)[G::SUB][G::KS]) {
+  auto load = [&](bool values, int x, ju4 (&d)[G::SUB][G::KS]) {
+    const PrefixSource &src = of_tail(x) ? a.tail : a.prefix;
+    const uint8_t *base = static_cast<const uint8_t *>(values ? src.V : src.K);
 #pragma unroll
     for (int u = 0; u < G::SUB; ++u)
 #pragma unroll
@@ -482,9 +515,9 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
   if (x0 < end) {
     ask_pages(x0);
     place(x0);
-    load(Kb, kr);
-    load(Vb, vr);
-    ask_pages(x0 + STRIDE);
+    load(false, x0, kr);
+    load(true, x0, vr);
+    if (x0 + STRIDE < end) ask_pages(x0 + STRIDE);
   }
   for (int x = x0; x < end; x += STRIDE) {
     f4_t s[G::SUB][NQ];
@@ -503,7 +536,7 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
       okm[u] = (uint32_t)__ballot(at[u].ok) & 0xffffu;
       whole &= okm[u] == 0xffffu;
     }
-    const bool partly = x + G::TPW > seen_all;   // some row does not see all of it
+    const bool tail = of_tail(x), partly = tail && x - tail0 + G::TPW > seen_all;   // some row does not see all of it
     bool mine[G::SUB];
 #pragma unroll
     for (int u = 0; u < G::SUB; ++u) mine[u] = at[u].ok;
@@ -511,8 +544,8 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
     const bool more = xn < end;
     if (more) {
       place(xn);
-      load(Kb, kr);
-      ask_pages(xn + STRIDE);
+      load(false, xn, kr);
+      if (xn + STRIDE < end) ask_pages(xn + STRIDE);
     }
     if (!whole || partly) {
 #pragma unroll
@@ -523,7 +556,7 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
           const bool there = (okm[u] >> k) & 1;
 #pragma unroll
           for (int q = 0; q < NQ; ++q)
-            if (!there || (TAIL && x + 16 * u + k >= R.seen[q])) s[u][q][i] = -INFINITY;
+            if (!there || (TAIL && tail && x - tail0 + 16 * u + k >= R.seen[q])) s[u][q][i] = -INFINITY;
         }
       // a value that is not there must not be NaN either
 #pragma unroll
@@ -552,7 +585,7 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
 #pragma unroll
         for (int k = 0; k < G::KS; ++k) bad |= nonfinite<T>(vr[u][k]);
       if (__any(bad)) {
-        R.template add_nonfinite<G::TPW>(vl, x, n16, g);
+        R.template add_nonfinite<G::TPW>(vl, x - tail0, n16, g);
 #pragma unroll
         for (int u = 0; u < G::SUB; ++u)
 #pragma unroll
@@ -560,11 +593,11 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
         put();
       }
     }
-    if (more) load(Vb, vr);
+    if (more) load(true, xn, vr);
     R.values(s, vl, n16, g);
   }
   const int64_t base = (int64_t)id * p.rows;
-  if constexpr (TAIL) {
+  if constexpr (OWN) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       const float l = over_groups_sum(R.l[q]);
@@ -602,8 +635,13 @@ JOLT_DEV void few(const PrefixAttendArgs &a, const FewArgs &p, int block, FewLds
         o += *reinterpret_cast<const f4_t *>(sm.w[w] + (row * D + e) * 4) * al;
       }
     }
-    *reinterpret_cast<f4_t *>(p.out.o + (base + row) * D + e) = o;
-    if (e == 0) p.out.ml[base + row] = make_float2(M, l);
+    if constexpr (WHOLE) {
+      const int t = t0 + row / a.group, j = h * a.group + row % a.group;
+      write_row<D, T>(a, t, j, e, o, M, l, e == 0);
+    } else {
+      *reinterpret_cast<f4_t *>(p.out.o + (base + row) * D + e) = o;
+      if (e == 0) p.out.ml[base + row] = make_float2(M, l);
+    }
   }
 }
 
@@ -834,8 +872,8 @@ __global__ void __launch_bounds__(NT, 2) k_runs(const RunArgs p) {
   __shared__ __attribute__((aligned(16))) RunLds<D, T> sm;
   int b = blockIdx.x;
   if (b < p.n_pre) {
-    if (p.pre_role == ROLE_FEW1) few<D, T, 1, false>(p.a, p.pre_few, b, sm.f1);
-    else if (p.pre_role == ROLE_FEW2) few<D, T, 2, false>(p.a, p.pre_few, b, sm.f2);
+    if (p.pre_role == ROLE_FEW1) few<D, T, 1, FEW_PREFIX>(p.a, p.pre_few, b, sm.f1);
+    else if (p.pre_role == ROLE_FEW2) few<D, T, 2, FEW_PREFIX>(p.a, p.pre_few, b, sm.f2);
     else if (p.pre_role == ROLE_MANY1) many<D, T, 1, false>(p.a, p.pre_many, b, sm.m);
     else many<D, T, 2, false>(p.a, p.pre_many, b, sm.m);
     return;
@@ -847,8 +885,15 @@ __global__ void __launch_bounds__(NT, 2) k_runs(const RunArgs p) {
     return;
   }
   b -= p.n_many;
-  if (p.few_role == ROLE_FEW1) few<D, T, 1, true>(p.a, p.few, b, sm.f1);
-  else few<D, T, 2, true>(p.a, p.few, b, sm.f2);
+  if (p.few_role == ROLE_FEW1) few<D, T, 1, FEW_TAIL>(p.a, p.few, b, sm.f1);
+  else few<D, T, 2, FEW_TAIL>(p.a, p.few, b, sm.f2);
+}
+
+// Short calls in one launch: a workgroup a request and key-value head, from the prefix to the output.
+template <int D, class T, int NQ>
+__global__ void __launch_bounds__(NT, 2) k_whole(const PrefixAttendArgs a) {
+  __shared__ __attribute__((aligned(16))) FewLds<D, T, NQ> sm;
+  few<D, T, NQ, FEW_WHOLE>(a, FewArgs{}, blockIdx.x, sm);
 }
 
 // ------------------------------------------------------------------------------- join
@@ -963,14 +1008,7 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
         for (int i = 0; i < 4; ++i) o[i] = fmaf(part[w][col + i], al, o[i]);
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (sub == 0) {
-    T *O = static_cast<T *>(a.O) + (int64_t)t * a.o_stride + (int64_t)j * D + col;
-    o *= inv;
-    if constexpr (sizeof(T) == 4) gstore_f4(O, o);
-    else *reinterpret_cast<uint2 *>(O) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
-  }
-  if (a.lse && gl == 0) a.lse[id] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
+  if (sub == 0) write_row<D, T>(a, t, j, col, o, M, l, gl == 0);
 }
 
 // ------------------------------------------------------------------------------- launches
@@ -1018,6 +1056,11 @@ hipError_t run(const PrefixAttendArgs &a, const PrefixCut &c, uint8_t *ws, hipSt
   auto parts = [&](size_t o, size_t m) { return Parts{reinterpret_cast<float *>(ws + o), reinterpret_cast<float2 *>(ws + m)}; };
   const Parts pp = parts(c.off_po, c.off_pm), pf = parts(c.off_fo, c.off_fm), pm = parts(c.off_mo, c.off_mm);
   RowEntry *entries = reinterpret_cast<RowEntry *>(ws + c.off_entries);
+  if (c.whole) {
+    if (c.few_nq == 1) k_whole<D, T, 1><<<a.n_req * a.heads, NT, 0, st>>>(a);
+    else k_whole<D, T, 2><<<a.n_req * a.heads, NT, 0, st>>>(a);
+    return hipGetLastError();
+  }
   RunArgs p{};
   p.a = a;
   if (a.T > 0 && c.prefix_few) {
@@ -1057,6 +1100,22 @@ hipError_t run(const PrefixAttendArgs &a, const PrefixCut &c, uint8_t *ws, hipSt
 PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype) {
   PrefixCut c;
   const int64_t rows = (int64_t)a.n_tok * a.group;     // rows of a key-value head
+  const int64_t most = (int64_t)a.max_new * a.group;   // rows of a request
+  // Requests as a whole save the join and its launch, but read the prefix once a request and leave
+  // all of a request and head to one workgroup: for those of few rows and up to 3 steps of its
+  // waves (128 tokens each, fp32 64), at most 4 steps counted once for every 256 workgroups.  In one
+  // launch and in two (us; d 128, bf16 and fp32):
+  //     32 workgroups, 3 steps  9.7 and 11.3, 11.5 and 13.8;  4 steps 11.7 and 11.4, 14.0 and 14.0
+  //    512 workgroups, 2 steps 11.4 and 13.6, 14.1 and 16.1;  3 steps 15.7 and 15.3, (4) 20.2 and 18.6
+  //   1024 workgroups, 1 step  14.7 and 15.8, 15.1 and 17.0;  2 steps 21.4 and 17.1, 25.7 and 20.9
+  const int64_t steps = ceil_div(a.T + ((int64_t)a.max_pages << a.tail.shift), WAVES * (dtype == JOLT_BF16 ? 32 : 16));
+  const int64_t whole = (int64_t)a.n_req * a.heads;    // workgroups that takes
+  if (most <= 32 && steps <= 3 && steps * ceil_div(whole, BLOCKS / 2) <= 4) {
+    c.whole = true;
+    c.few_nq = most <= 16 ? 1 : 2;
+    c.ws_bytes = 256;
+    return c;
+  }
   if (a.T > 0) {
     // Up to 32 rows few() reads the prefix at the rate of memory: 32 rows on 32768 tokens of 8 heads
     // take 38 us, 44 by many(); 17 rows on 4001 tokens of 40 heads 29 and 32.
@@ -1075,7 +1134,6 @@ PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype) {
   if (a.max_pages > 0) {
     // Requests of up to 32 rows by few(), also where that takes two groups of rows a wave: 64 requests
     // of up to 32 rows and 500 tokens take 22 us, 26 with those past 16 rows by many() (fp32 33, 64).
-    const int64_t most = (int64_t)a.max_new * a.group; // rows of a request
     c.few_nq = most <= 16 ? 1 : 2;
     c.limit = 16 * c.few_nq;
     c.few_rows = (int)std::min<int64_t>(most, c.limit);

@@ -274,6 +274,7 @@ struct PrefixAttendArgs {
 };
 // How a call is cut into runs, from its sizes alone, and where its workspace keeps their results.
 struct PrefixCut {
+  bool whole = false;                                            // a request a workgroup and head, one launch
   bool prefix_few = false, tails_many = false;
   int32_t prefix_nq = 1, prefix_run = 0, n_prefix = 0;           // few(): tokens of a run; runs of a row
   int32_t prefix_tiles = 0, prefix_groups = 0, kv_tiles = 0;     // many(): row tiles, workgroups of a head

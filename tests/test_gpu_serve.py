@@ -255,7 +255,7 @@ CASES = [  # T, have, new, H, G, d, page
     (513, [0, 200], [40, 70], 2, 3, 64, 16), (260, [9, 0, 0, 50], [1, 130, 0, 7], 2, 8, 32, 128),
     (64, [1, 2, 3], [16, 17, 15], 4, 1, 128, 1024), (0, [700, 0, 5], [1, 33, 2], 1, 16, 64, 32),
     (2050, [300], [1], 1, 64, 128, 16), (33, [4] * 70, [1] * 70, 1, 2, 64, 4),
-    (700, [20, 0, 33], [8, 5, 7], 40, 4, 128, 16), (129, [2, 500], [1, 25], 16, 1, 32, 16),
+    (700, [20, 0, 33], [8, 5, 7], 40, 4, 128, 16), (400, [31, 0, 32, 1, 63], [1, 2, 8, 1, 3], 2, 4, 32, 32), (0, [0, 1, 31, 32, 33], [1] * 5, 3, 2, 128, 8), (129, [2, 500], [1, 25], 16, 1, 32, 16),
 ]
 
 
@@ -298,9 +298,14 @@ def test_prefix_attend_rows_that_attend_to_nothing(dtype, new):
     want = b.want()
     assert np.isneginf(want[1]).any()
     b.check(b.run(max_new=max(new)), want)
-    b = Batch(dtype, 70, [0, 5, 0, 9], new, 2, 4, 64, 8)
-    b.kv_len = np.array([0, 0, 0, 0])
-    b.check(b.run(), b.want())
+    for T in (70, 700):
+        b = Batch(dtype, T, [0, 5, 0, 9], new, 2, 4, 64, 8)
+        for lens in ([0, 0, 0, 0], [1, 3, 0, 2]):
+            b.kv_len = np.minimum(lens, b.kv_len)
+            b.check(b.run(max_new=max(new)), b.want())
+    b = Batch(dtype, 0, [600, 5, 0, 9], new, 2, 4, 64, 8)     # a table with room for many pages
+    b.kv_len = np.minimum(b.kv_len, [600, 3, 1, 0])
+    b.check(b.run(max_new=max(new)), b.want())
 
 
 @pytest.mark.parametrize("layout", ["phd", "kv"])
@@ -312,20 +317,21 @@ def test_prefix_attend_layouts_of_pages(layout):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), "lowest"])
+@pytest.mark.parametrize("T", [50, 600])
 @pytest.mark.parametrize("new,d", [([1, 1, 1], 64), ([3, 2, 3], 32), ([7, 5, 8], 128), ([40, 2, 37], 64), ([33, 1, 90], 128)])
-def test_prefix_attend_ignores_what_a_row_does_not_attend_to(dtype, bad, new, d):
+def test_prefix_attend_ignores_what_a_row_does_not_attend_to(dtype, bad, new, d, T):
     """Whatever stands in unused page slots, behind the lengths and, for the rows before it, in the last token."""
     bad = float(torch.finfo(DT[dtype][1]).min) if bad == "lowest" else bad
-    b = Batch(dtype, 50, [60, 5, 17], new, 2, 4, d, 16, hole=bad)
-    want = b.want()
-    b.check(b.run(), want)
+    b = Batch(dtype, T, [60, 5, 17], new, 2, 4, d, 16, hole=bad)
+    want, m = b.want(), max(new)
+    b.check(b.run(max_new=m), want)
     # the last token of request 0: keys first, then values; every row but the last is as before
     r, last = 0, int(b.kv_len[0]) - 1
     keep = np.ones(b.n_tok, bool)
     keep[b.q_start[1] - 1] = False
     for pool in (b.Kp, b.Vp):
         pool[b.table[r, last // 16], :, last % 16] = bad
-        O, lse = b.run()
+        O, lse = b.run(max_new=m)
         for x, y in ((O, want[0]), (lse, want[1])):
             assert np.isfinite(x[keep]).all()
         b2 = [w.copy() for w in want]
@@ -334,11 +340,11 @@ def test_prefix_attend_ignores_what_a_row_does_not_attend_to(dtype, bad, new, d)
 
 
 def test_prefix_attend_value_that_is_not_finite_reaches_the_rows_that_see_it():
-    for new in ([1, 1], [4, 40]):
-        b = Batch("bf16", 50, [60, 5], new, 2, 4, 64, 16)
+    for new, T in (([1, 1], 50), ([4, 40], 50), ([1, 1], 600), ([4, 2], 50), ([4, 2], 600)):
+        b = Batch("bf16", T, [60, 5], new, 2, 4, 64, 16)
         b.V[1, 1, 7, 3] = float("inf")
         b.Vp[b.table[0, 0], 0, 2, 5] = float("nan")
-        O, _ = b.run()
+        O, _ = b.run(max_new=max(new))
         n0 = int(b.q_start[1])
         assert np.isposinf(O[:, 4:, 3]).all() and np.isfinite(np.delete(O[:, 4:], 3, 2)).all()
         assert np.isnan(O[:n0, :4, 5]).all() and np.isfinite(O[n0:, :4]).all() and np.isfinite(np.delete(O[:, :4], 5, 2)).all()
@@ -354,10 +360,10 @@ def test_prefix_attend_scores_far_apart():
 
 
 def test_prefix_attend_leaves_rows_behind_the_last_request():
-    for new in ([1, 0, 1], [30, 2, 0]):
-        b = Batch("bf16", 100, [60, 5, 17], new, 2, 4, 128, 16, pad_rows=37)
+    for new, T in (([1, 0, 1], 100), ([30, 2, 0], 100), ([1, 0, 1], 1000)):
+        b = Batch("bf16", T, [60, 5, 17], new, 2, 4, 128, 16, pad_rows=37)
         b.Q[b.q_start[-1]:] = float("nan")
-        b.check(b.run(), b.want())
+        b.check(b.run(max_new=max(new)), b.want())
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -377,8 +383,8 @@ def test_prefix_attend_rows_do_not_depend_on_their_neighbours(dtype):
 def test_prefix_attend_bounds_lengths_and_pages_that_are_wrong():
     """Lengths past the table, pages outside the pool, starts past the rows: nothing outside is
     read or written (checked on the rows that are still well defined)."""
-    for new in ([1, 1, 1], [20, 2, 3]):
-        b = Batch("bf16", 40, [60, 5, 17], new, 2, 4, 64, 16)
+    for new, T in (([1, 1, 1], 40), ([20, 2, 3], 40), ([1, 1, 1], 640)):
+        b = Batch("bf16", T, [60, 5, 17], new, 2, 4, 64, 16)
         want = b.want()
         b.table[1] = [-1] * b.table.shape[1]
         b.table[2, 0] = b.desc.n_pages
