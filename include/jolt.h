@@ -498,7 +498,8 @@ typedef struct {
  *              0..n_pages - 1 are not attended to.
  * Q, O ([n_tok][n_q][d]), prefix and pages are of one type.  bf16: the products are of bf16
  * values summed in fp32, scores and softmax in fp32, the softmax weights rounded to bf16 for
- * the value product, O rounded once.  fp32: fp32 throughout.  Results do not depend on the
+ * the value product, O rounded once.  fp32: fp32 throughout.  Where the sum of |v_x| over the
+ * tokens that a row attends to is within fp32, O is finite.  Results do not depend on the
  * order of arrival of anything (no atomics): equal calls give equal bits.
  * O and lse overlap no input.  At most 1024 key-value heads, n_tok * n_q < 2^28.  ws: device, 256-byte aligned, at least
  * jolt_prefix_attend_workspace_size bytes, not shared by calls that may run at the same time.

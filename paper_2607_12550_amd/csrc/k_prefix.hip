@@ -234,10 +234,15 @@ struct Rows {
     }
   }
   // Scores s (16 SUBS tokens) into weights, in place.  The reference m of exp2(s c - m) need not
-  // be the running maximum, only near it: it is kept while a lane's weights sum to at most 2^16
-  // (nothing is near overflow then, and a weight's precision does not depend on its size), so
-  // that most tiles need no maximum, no exchange between lanes and no rescaling.  The first tile
-  // (m = -inf gives an infinite sum) and one that outgrows m take the maximum and rescale.
+  // be the running maximum, only near it: it is kept while a lane's weights of a step sum to at most
+  // 1 (a weight's precision does not depend on its size), so that most tiles need no maximum, no
+  // exchange between lanes and no rescaling.  The first tile (m = -inf gives an infinite sum) and
+  // one that outgrows m set it HEAD above the maximum and rescale: weights then start at 2^-8, and
+  // what follows may score 8 higher before m moves again.  No weight is ever above 1, so that sums
+  // of values overflow only where those of the plain softmax could; with the maximum itself as
+  // reference and weights of up to 2^16, values of 1e37 gave infinite sums.  Values below 2^-118 meet
+  // weights small enough to lose bits of fp32 (never those of bf16); with 2^-16 those below 2^-110 did.
+  static constexpr float HEAD = 8.f;
   template <int SUBS>
   JOLT_DEV void softmax(f4_t (&s)[SUBS][NQ], float c) {
     f4_t p[SUBS][NQ];
@@ -257,17 +262,17 @@ struct Rows {
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       weigh(x);
-      far |= !(sum[x] <= 65536.f) || m[x] == -INFINITY;
+      far |= !(sum[x] <= 1.f) || m[x] == -INFINITY;
     }
     if (__builtin_expect(__any(far), 0)) {
 #pragma unroll
       for (int x = 0; x < NQ; ++x) {
         // only where this query's own lanes say so: no row's rounding depends on another's values
-        const bool mine = !(sum[x] <= 65536.f) || m[x] == -INFINITY;
+        const bool mine = !(sum[x] <= 1.f) || m[x] == -INFINITY;
         float mx = max4(s[0][x]);
 #pragma unroll
         for (int u = 1; u < SUBS; ++u) mx = fmaxf(mx, max4(s[u][x]));
-        mx = fmaxf(m[x], over_groups_max(mx) * c);
+        mx = fmaxf(m[x], over_groups_max(mx) * c + HEAD);
         if (over_groups_max(mine ? 1.f : 0.f) == 0.f) mx = m[x];
         // nothing seen so far: both are -inf, and nothing is there to rescale
         const float al = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[x] - mx);
