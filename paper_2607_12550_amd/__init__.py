@@ -475,9 +475,7 @@ def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, k
     have, add, kv_len [n_req]; q_start [n_req + 1]; table [n_req, max_pages]; slots, positions
     [n_tok]; n_free, n_free_out [1]; info [4]."""
     n, n_tok, cap = have.numel(), slots.numel(), free_pages.numel()
-    if table.dim() != 2 or table.shape[0] != n:
-        raise ValueError("table must be [n_req, max_pages]")
-    columns = table.shape[1]
+    columns = _marshal.columns(table, n, "table")
     h, ad, fr, nf, tb, kv, qs, sl, po, no, inf = _marshal.flat(
         "int32", have, n, "have", add, n, "add", free_pages, cap, "free_pages", n_free, 1, "n_free", table, n * columns, "table",
         kv_len, n, "kv_len", q_start, n + 1, "q_start", slots, n_tok, "slots", positions, n_tok, "positions",
@@ -487,15 +485,17 @@ def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, k
 
 def jolt_page_append(ctx, pages: PageDesc, K, V, slots, K_pages, V_pages, positions=None, rope=None, stream=None) -> None:
     """Writes the rows K, V [n_tok, n_heads, d] into their slots of the pools; rope: None, or
-    (base, position_offset) to rotate the keys at positions + position_offset."""
+    (base, position_offset) to rotate the keys at positions + position_offset.  The pools are tensors of the
+    descriptor's type whose memory holds all of its pages, or addresses."""
     n, bf16, heads, d = slots.numel(), pages.dtype == JOLT_BF16, pages.n_heads, pages.d
+    kp, vp = _marshal.pools(pages, K_pages, V_pages)
     k, _, _, k_token, k_head = _marshal.rows(K, bf16, n, heads, d, "K")
     v, _, _, v_token, v_head = _marshal.rows(V, bf16, n, heads, d, "V")
     sl, = _marshal.flat("int32", slots, n, "slots")
     po = 0 if positions is None else _marshal.flat("int32", positions, n, "positions")[0]
     r = None if rope is None else Rope(float(rope[0]), int(rope[1]), 0)
     _check(lib.jolt_page_append(ctx, pages, n, sl, po, r, k, RowStrides(k_token, k_head), v, RowStrides(v_token, v_head),
-                                _addr(K_pages), _addr(V_pages), _stream(stream)))
+                                kp, vp, _stream(stream)))
 
 
 def jolt_prefix_attend_workspace_size(n_req: int, n_tok: int, n_q: int, prefix=None, pages=None, max_pages: int = 0,
@@ -514,30 +514,31 @@ def jolt_prefix_attend(ctx, Q, O, q_start, kv_len, scale: float, ws, prefix=None
     """Attention of the packed rows Q [n_tok, n_q, d] of a batch over the prefix its requests
     share (layer `layer` of the cell `prefix`) and each request's own pages; writes O and, if
     given, lse [n_tok, n_q] fp32.  q_start [n_req + 1], kv_len [n_req], table [n_req, max_pages]
-    are device int32 tensors."""
+    are device int32 tensors.  Cell, pools and workspace are tensors whose memory holds what their
+    descriptors (ws: ws_bytes, or its own size) reach, of the descriptors' type, or addresses."""
     n_req = q_start.numel() - 1
     desc = pages if pages is not None else prefix
     if desc is None:
         raise ValueError("a prefix or pages are needed")
     d, bf16 = desc.d, desc.dtype == JOLT_BF16
+    kc, vc = (0, 0) if prefix is None else _marshal.cell(prefix, layer, K_prefix, V_prefix)
+    w, wsb = _marshal.bytes(ws, ws_bytes, "ws")
     q, n_tok, n_q, q_token, q_head = _marshal.rows(Q, bf16, -1, -1, d, "Q")
     o, _, _, o_token, o_head = _marshal.rows(O, bf16, n_tok, n_q, d, "O")
     if n_q > 1 and (q_head != d or o_head != d):
         raise ValueError("the heads of a row of Q and O must be contiguous")
     ls = 0 if lse is None else _marshal.flat("float32", lse, n_tok * n_q, "lse")[0]
-    columns, tab, lens = 0, 0, 0
+    columns, tab, lens, kp, vp = 0, 0, 0, 0, 0
     if pages is not None:
-        if table.dim() != 2 or table.shape[0] != n_req:
-            raise ValueError("table must be [n_req, max_pages]")
-        columns = table.shape[1]
+        kp, vp = _marshal.pools(pages, K_pages, V_pages)
+        columns = _marshal.columns(table, n_req, "table")
         starts, tab, lens = _marshal.flat("int32", q_start, n_req + 1, "q_start", table, n_req * columns, "table", kv_len, n_req, "kv_len")
     else:
         starts, = _marshal.flat("int32", q_start, n_req + 1, "q_start")
     row = n_q * d
     b = AttendBatch(n_req, n_tok, n_q, columns, max_new, 0, q_token if n_tok > 1 else row, o_token if n_tok > 1 else row)
-    wsb = ws_bytes if ws_bytes is not None else (ws.numel() * ws.element_size())
-    _check(lib.jolt_prefix_attend(ctx, prefix, _addr(K_prefix), _addr(V_prefix), layer, pages, _addr(K_pages), _addr(V_pages), tab, b,
-                                  starts, lens, q, float(scale), o, ls, _addr(ws), wsb, _stream(stream)))
+    _check(lib.jolt_prefix_attend(ctx, prefix, kc, vc, layer, pages, kp, vp, tab, b,
+                                  starts, lens, q, float(scale), o, ls, w, wsb, _stream(stream)))
 
 
 def jolt_debug_export(ctx, what: int, cell: int, dst, stream=None) -> None:

@@ -1,0 +1,77 @@
+"""Host-side checks of the shared-prefix serving operators at the edges of what they accept (no GPU
+needed): tensors that do not hold what a descriptor reaches.
+"""
+import pytest
+import torch
+
+import paper_2607_12550_amd as J
+from test_host_serve import A, _pages, _prefix
+
+
+def _small(**kw):
+    """Pages of 2 heads, 4 tokens and 32 features, 3 of them: 768 elements."""
+    return _pages(**{**dict(n_heads=2, page_size=4, d=32, n_pages=3, stride_page=256, stride_head=128, stride_token=32), **kw})
+
+
+def _cell(**kw):
+    """Two layers of 2 heads, 5 tokens and 32 features: 640 elements, 320 of them for layer 0 alone."""
+    return _prefix(**{**dict(n_layers=2, n_heads=2, T=5, d=32, stride_layer=320, stride_head=160, stride_token=32), **kw})
+
+
+def _t(n, dtype=torch.bfloat16):
+    return torch.zeros(n, dtype=dtype)
+
+
+def test_memory_that_a_descriptor_reaches_is_checked():
+    """Type, size and device of pools, prefix and workspace; a host tensor is the last to be seen, so
+    one that fits in all else shows that."""
+    big = torch.zeros(1000, dtype=torch.bfloat16)
+    for bad, word in ((_t(768, torch.float32), "bfloat16"), (_t(767), "768 elements"), (big[300:], "768 elements"),
+                      (_t(1).expand(768), "768 elements"), (_t(768), "on the GPU"), (big[232:], "on the GPU"), ([1], "must be a tensor")):
+        for K, V, name in ((bad, A, "K_pages"), (A, bad, "V_pages")):
+            with pytest.raises(ValueError, match=name) as e:
+                J._marshal.pools(_small(), K, V)
+            assert word in str(e.value)
+    # padded rows, tokens outside heads, and strides of axes of one element, which reach nowhere
+    for desc, n in ((_small(stride_token=40, stride_head=160, stride_page=320), 2 * 320 + 160 + 3 * 40 + 32),
+                    (_small(stride_token=64, stride_head=32), 768), (_small(n_pages=1, stride_page=1 << 40), 256)):
+        with pytest.raises(ValueError, match=f"{n} elements"):
+            J._marshal.pools(desc, _t(n - 1), A)
+        with pytest.raises(ValueError, match="on the GPU"):
+            J._marshal.pools(desc, _t(n), A)
+    with pytest.raises(ValueError, match="float32"):
+        J._marshal.pools(_small(dtype=J.JOLT_F32), _t(768), A)
+    for layer, n in ((0, 320), (1, 640), (5, 320)):
+        with pytest.raises(ValueError, match="K_prefix.*%d elements" % n):
+            J._marshal.cell(_cell(), layer, _t(n - 1), A)
+        with pytest.raises(ValueError, match="V_prefix.*on the GPU"):
+            J._marshal.cell(_cell(), layer, A, _t(n))
+    assert J._marshal.pools(_small(), A, None) == (A, 0) and J._marshal.cell(_cell(), 0, None, A) == (0, A)
+
+
+def test_workspaces_are_checked():
+    ws = torch.zeros(256, dtype=torch.uint8)
+    for a, size, word in ((ws, 257, "257 bytes"), (ws[1:], 256, "256 bytes"), (ws[:1].expand(1 << 20), None, "bytes"), (ws, None, "on the GPU"),
+                          (ws.float(), 1024, "on the GPU"), (A, None, "size"), (None, None, "must be a tensor"), (A, -1, "negative")):
+        with pytest.raises(ValueError, match=word):
+            J._marshal.bytes(a, size, "ws")
+    assert J._marshal.bytes(A, 77, "ws") == (A, 77) and J._marshal.bytes(None, 77, "ws") == (0, 77)
+
+
+def test_host_pools_prefix_and_workspace_never_reach_a_kernel():
+    """The public calls look at the memory that they are given before anything else."""
+    z = torch.zeros(4, dtype=torch.int32)
+    rows = torch.zeros((4, 2, 32), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="V_pages must be a tensor on the GPU"):
+        J.jolt_page_append(None, _small(), rows, rows, z, A, _t(768))
+    ok = dict(prefix=_cell(), K_prefix=A, V_prefix=2 * A, pages=_small(), K_pages=3 * A, V_pages=4 * A, table=torch.zeros((3, 2), dtype=torch.int32),
+              ws_bytes=256)
+    for kw, ws, word in ((dict(K_prefix=_t(640)), A, "K_prefix must"), (dict(), _t(256, torch.uint8), "ws must")):
+        with pytest.raises(ValueError, match=word):
+            J.jolt_prefix_attend(None, rows, rows, z, z[:3], 0.1, ws, **{**ok, **kw})
+    with pytest.raises(ValueError, match="table must be a tensor"):
+        J._marshal.columns(None, 3, "table")
+    for t in (z, ok["table"][:2]):
+        with pytest.raises(ValueError, match="n_req, max_pages"):
+            J._marshal.columns(t, 3, "table")
+    assert J._marshal.columns(ok["table"], 3, "table") == 2
