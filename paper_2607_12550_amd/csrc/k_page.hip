@@ -155,7 +155,9 @@ __global__ void __launch_bounds__(NT) k_page_append(const PageAppendArgs a) {
   constexpr int E = 16 / sizeof(T);        // elements of a 16-byte piece
   constexpr int C = D / E, HALF = D / 2;
   __shared__ float2 cs[HALF];
-  const int t = blockIdx.x, tid = threadIdx.x;
+  const uint32_t t = blockIdx.y * gridDim.x + blockIdx.x;
+  const int tid = threadIdx.x;
+  if (t >= (uint32_t)a.n_tok) return;
   const int slot = a.slots[t];
   if (slot < 0 || slot >= a.n_slots) return;
   const int64_t at = (int64_t)(slot >> a.page_shift) * a.s_page + (int64_t)(slot & ((1 << a.page_shift) - 1)) * a.s_tok;
@@ -201,10 +203,11 @@ __global__ void __launch_bounds__(NT) k_page_append(const PageAppendArgs a) {
 
 template <int D>
 hipError_t append(const PageAppendArgs &a, int dtype, hipStream_t st) {
+  const dim3 grid = grid_of(a.n_tok);
   if (dtype == JOLT_BF16)
-    k_page_append<D, bf16_t><<<a.n_tok, NT, 0, st>>>(a);
+    k_page_append<D, bf16_t><<<grid, NT, 0, st>>>(a);
   else
-    k_page_append<D, float><<<a.n_tok, NT, 0, st>>>(a);
+    k_page_append<D, float><<<grid, NT, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -252,6 +252,12 @@ struct PageAppendArgs {
   int32_t rope, offset;
   double turns[64];                            // base^(-2 j / d) / (2 pi): turns per position
 };
+// A launch takes below 2^32 threads along an axis: more workgroups continue along the second, as
+// number blockIdx.y * gridDim.x + blockIdx.x, with up to 2^22 - 1 too many at the end.
+inline dim3 grid_of(int64_t workgroups) {
+  const int64_t row = (int64_t)1 << 22;
+  return workgroups <= row ? dim3((uint32_t)workgroups) : dim3((uint32_t)row, (uint32_t)((workgroups + row - 1) / row));
+}
 hipError_t launch_page_append(const PageAppendArgs &a, int d, int dtype, hipStream_t st);
 
 // Where the rows of keys and values lie: token x of a run sits at

@@ -1,10 +1,13 @@
 """GPU tests of the shared-prefix serving operators at the edges of what they accept: values near
-the largest of their type.  Oracle and tolerances are those of test_gpu_serve.py.
+the largest of their type, and more rows than one axis of a launch takes.  Oracle and
+tolerances are those of test_gpu_serve.py.
 """
 import pytest
 import torch
 
-from test_gpu_serve import Batch
+import paper_2607_12550_amd as J
+from gpu_util import ctx, note
+from test_gpu_serve import Batch, dev_i, pages_desc
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +29,22 @@ def test_large_values_under_rising_scores(dtype, new, T):
         b.K[1] = u * torch.linspace(0.05, 2.5, T, device="cuda")[None, :, None] + 0.02 * b.K[1].float()
         b.Q.copy_(u + 0.1 * b.Q.float())
         b.check(b.run(max_new=max(new)), b.want())
+
+
+def test_append_of_more_rows_than_a_launch_axis_takes():
+    """2^24 and more rows of one head; rows at both ends and around the axis's length have slots."""
+    n = (1 << 24) + 5
+    at = torch.tensor([0, 1, (1 << 22) - 1, 1 << 22, (1 << 23) + 7, (1 << 24) - 1, 1 << 24, n - 1], device="cuda")
+    desc = pages_desc("bf16", 1, 8, 32, 2)
+    K = torch.zeros((n, 1, 32), dtype=torch.bfloat16, device="cuda")
+    K[at] = torch.randn((8, 1, 32), device="cuda", generator=torch.Generator("cuda").manual_seed(0)).bfloat16()
+    slots = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    slots[at] = dev_i(range(3, 11))
+    Kp, Vp = (torch.full((2, 1, 8, 32), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    note("jolt_page_append", n)
+    J.jolt_page_append(ctx(), desc, K, K[:1].expand(n, 1, 32), slots, Kp, Vp)
+    torch.cuda.synchronize()
+    kp, vp = Kp.view(16, 32), Vp.view(16, 32)
+    assert torch.equal(kp[3:11], K[at, 0]) and torch.equal(vp[3:11], K[:1, 0].expand(8, 32))
+    for x in (kp, vp):
+        assert (x[:3] == 3).all() and (x[11:] == 3).all()
