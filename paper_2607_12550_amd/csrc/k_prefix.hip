@@ -924,7 +924,8 @@ __global__ void __launch_bounds__(NT) k_join(const JoinArgs p) {
   __shared__ float part[BLOCK ? WAVES : 1][D + 2];
   const PrefixAttendArgs &a = p.a;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, gl = lane % LW, sub = gl / LR, col = 4 * (gl % LR);
-  const int id = BLOCK ? (int)blockIdx.x : (int)blockIdx.x * (NT / LW) + (int)threadIdx.x / LW;
+  const int block = blockIdx.y * gridDim.x + blockIdx.x;
+  const int id = BLOCK ? block : block * (NT / LW) + (int)threadIdx.x / LW;
   if (id >= a.n_tok * a.n_q) return;
   const int t = id / a.n_q, j = id - t * a.n_q, h = j / a.group, jj = j - h * a.group;
   RowEntry e = p.entries[t];
@@ -1093,7 +1094,7 @@ hipError_t run(const PrefixAttendArgs &a, const PrefixCut &c, uint8_t *ws, hipSt
   // runs: 11 us by D / 4 lanes, 14 by waves; 2048 rows of 11: 7.3 and 6.0; 384 rows of 171: 9 us by
   // waves, 6 by workgroups).
   const int64_t out_rows = (int64_t)a.n_tok * a.n_q;
-  auto grid = [&](int lanes) { return (int)ceil_div(out_rows * lanes, NT); };
+  auto grid = [&](int lanes) { return grid_of(ceil_div(out_rows * lanes, NT)); };
   if (out_rows <= 2 * BLOCKS) k_join<D, T, 64, true><<<grid(NT), NT, 0, st>>>(j);
   else if (out_rows <= 8 * BLOCKS) k_join<D, T, 64, false><<<grid(64), NT, 0, st>>>(j);
   else k_join<D, T, D / 4, false><<<grid(D / 4), NT, 0, st>>>(j);

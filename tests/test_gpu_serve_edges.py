@@ -48,3 +48,24 @@ def test_append_of_more_rows_than_a_launch_axis_takes():
     assert torch.equal(kp[3:11], K[at, 0]) and torch.equal(vp[3:11], K[:1, 0].expand(8, 32))
     for x in (kp, vp):
         assert (x[:3] == 3).all() and (x[11:] == 3).all()
+
+
+def test_attention_of_more_rows_than_a_launch_axis_takes():
+    """2^27 and more output rows of 128 features: with queries of zero over one token of prefix every
+    row is that token's value, exactly.  The workspace is about 70 GB, the rows twice 34."""
+    n_tok, n_q, d = (1 << 21) + 1, 64, 128
+    prefix = J.cell_desc(dtype=J.JOLT_BF16, n_layers=1, n_heads=1, T=1, d=d, stride_layer=d, stride_head=d, stride_token=d)
+    nb = J.jolt_prefix_attend_workspace_size(1, n_tok, n_q, prefix=prefix)
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < nb + 4 * n_tok * n_q * d + (8 << 30):
+        pytest.skip("needs about 150 GB of free device memory")
+    K, V = torch.randn((2, d), device="cuda", generator=torch.Generator("cuda").manual_seed(0)).bfloat16()
+    Q = torch.zeros((n_tok, n_q, d), dtype=torch.bfloat16, device="cuda")
+    O, ws = torch.full_like(Q, 9.0), torch.empty(nb, dtype=torch.uint8, device="cuda")
+    note("jolt_prefix_attend", n_tok, n_q, d, nb)
+    J.jolt_prefix_attend(ctx(), Q, O, dev_i([0, n_tok]), None, 0.1, ws, prefix=prefix, K_prefix=K, V_prefix=V)
+    torch.cuda.synchronize()
+    right = all(bool((O[t:t + (1 << 16)] == V).all()) for t in range(0, n_tok, 1 << 16))
+    del Q, O, ws
+    torch.cuda.empty_cache()
+    assert right
