@@ -47,6 +47,7 @@ JOLT_EXACT, JOLT_FLASH = 0, 1
 JOLT_FACTOR_F32, JOLT_FACTOR_F16 = 0, 1
 JOLT_PLAN_NO_PAGES, JOLT_PLAN_TABLE_FULL, JOLT_PLAN_NO_TOKENS, JOLT_PLAN_BAD_LENGTH = 1, 2, 4, 8
 HEADER_BYTES = 128
+_INT_MAX = 2 ** 31 - 1
 
 
 class JoltError(RuntimeError):
@@ -475,6 +476,8 @@ def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, k
     have, add, kv_len [n_req]; q_start [n_req + 1]; table [n_req, max_pages]; slots, positions
     [n_tok]; n_free, n_free_out [1]; info [4]."""
     n, n_tok, cap = have.numel(), slots.numel(), free_pages.numel()
+    if max(n_tok, cap) > _INT_MAX:
+        raise ValueError("slots and free_pages hold at most 2^31 - 1 elements")
     columns = _marshal.columns(table, n, "table")
     h, ad, fr, nf, tb, kv, qs, sl, po, no, inf = _marshal.flat(
         "int32", have, n, "have", add, n, "add", free_pages, cap, "free_pages", n_free, 1, "n_free", table, n * columns, "table",
@@ -488,6 +491,8 @@ def jolt_page_append(ctx, pages: PageDesc, K, V, slots, K_pages, V_pages, positi
     (base, position_offset) to rotate the keys at positions + position_offset.  The pools are tensors of the
     descriptor's type whose memory holds all of its pages, or addresses."""
     n, bf16, heads, d = slots.numel(), pages.dtype == JOLT_BF16, pages.n_heads, pages.d
+    if n > _INT_MAX:
+        raise ValueError("slots hold at most 2^31 - 1 elements")
     kp, vp = _marshal.pools(pages, K_pages, V_pages)
     k, _, _, k_token, k_head = _marshal.rows(K, bf16, n, heads, d, "K")
     v, _, _, v_token, v_head = _marshal.rows(V, bf16, n, heads, d, "V")

@@ -215,7 +215,7 @@ hipError_t append(const PageAppendArgs &a, int dtype, hipStream_t st) {
 
 hipError_t launch_page_plan(const PagePlanArgs &a, hipStream_t st) {
   const size_t lds = (3 * a.n_req + 1) * sizeof(int32_t);
-  auto grid = [&](int step) { return (a.n_tok + step * NT - 1) / (step * NT); };
+  auto grid = [&](int step) { return (uint32_t)(((int64_t)a.n_tok + step * NT - 1) / (step * NT)); };
   if (a.n_tok <= 256 * NT) k_page_plan<1><<<grid(1), NT, lds, st>>>(a);
   else k_page_plan<4><<<grid(4), NT, lds, st>>>(a);
   return hipGetLastError();

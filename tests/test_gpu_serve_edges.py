@@ -1,6 +1,6 @@
 """GPU tests of the shared-prefix serving operators at the edges of what they accept: values near
-the largest of their type, and more rows than one axis of a launch takes.  Oracle and
-tolerances are those of test_gpu_serve.py.
+the largest of their type, and as many rows as an int counts.  Oracle and tolerances are those of
+test_gpu_serve.py.
 """
 import pytest
 import torch
@@ -69,3 +69,35 @@ def test_attention_of_more_rows_than_a_launch_axis_takes():
     del Q, O, ws
     torch.cuda.empty_cache()
     assert right
+
+
+def test_plan_of_as_many_rows_as_an_int_counts():
+    """2^31 - 1 packed rows, three quarters of them of requests."""
+    page, n_tok, cols = 1024, 2 ** 31 - 1, 1 << 19
+    have, add = [0, 1023, 5], [1 << 29, (1 << 29) - 1023, (1 << 29) - 100]
+    n_pages = 3 * cols
+    free = torch.randperm(n_pages, device="cuda", generator=torch.Generator("cuda").manual_seed(0)).to(torch.int32)
+    table = torch.full((3, cols), -1, dtype=torch.int32, device="cuda")
+    table[1, 0], table[2, 0] = free[-1], free[-2]
+    desc = pages_desc("bf16", 1, page, 32, n_pages)
+    torch.cuda.empty_cache()
+    slots, pos = (torch.full((n_tok,), 7, dtype=torch.int32, device="cuda") for _ in range(2))
+    kv, qs, left, info = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (3, 4, 1, 4))
+    note("jolt_page_plan", n_tok)
+    J.jolt_page_plan(ctx(), desc, dev_i(have), dev_i(add), free, dev_i([n_pages - 2]), table, kv, qs, slots, pos, left, info)
+    torch.cuda.synchronize()
+    starts = [0, add[0], add[0] + add[1], sum(add)]
+    assert qs.tolist() == starts and kv.tolist() == [h + n for h, n in zip(have, add)]
+    # each takes the pages that it does not hold, in order, from the top down
+    want = torch.cat([free[:-2].flip(0)[:cols], free[-1:], free[:-2].flip(0)[cols:2 * cols - 1], free[-2:-1], free[:-2].flip(0)[2 * cols - 1:]])
+    assert torch.equal(table.view(-1), want) and info.tolist() == [sum(add), n_pages - 2, 0, n_pages - 2] and left.tolist() == [0]
+    step = 1 << 27
+    for r in range(3):
+        for t in range(starts[r], starts[r + 1], step):
+            p = torch.arange(t, min(t + step, starts[r + 1]), device="cuda") - starts[r] + have[r]
+            assert torch.equal(pos[t:t + p.numel()], p.int())
+            assert torch.equal(slots[t:t + p.numel()], (table[r, p // page] * page + p % page).int())
+    for x in (slots, pos):
+        assert all(bool((x[t:t + step] == -1).all()) for t in range(sum(add), n_tok, step))
+    del slots, pos
+    torch.cuda.empty_cache()
