@@ -501,8 +501,11 @@ typedef struct {
  * the value product, O rounded once.  fp32: fp32 throughout.  Where the sum of |v_x| over the
  * tokens that a row attends to is within fp32, O is finite.  Results do not depend on the
  * order of arrival of anything (no atomics): equal calls give equal bits.
- * O and lse overlap no input.  At most 1024 key-value heads, n_tok * n_q < 2^28.  ws: device, 256-byte aligned, at least
- * jolt_prefix_attend_workspace_size bytes, not shared by calls that may run at the same time.
+ * O and lse overlap no input.  At most 1024 key-value heads, n_tok * n_q < 2^28.  ws: device,
+ * 256-byte aligned, at least jolt_prefix_attend_workspace_size bytes, not shared by calls that may
+ * run at the same time.  The size for a batch is enough for every one with the same heads, d and
+ * type and no more requests, rows, rows of a request (max_new, where 0 counts as n_tok), room in
+ * the table and tokens of prefix, so that a server allocates once, for its largest.
  * Errors: JOLT_E_INVAL, JOLT_E_UNSUPPORTED, JOLT_E_WORKSPACE. */
 int jolt_prefix_attend_workspace_size(const jolt_cell_desc *prefix, const jolt_page_desc *pages,
                                       const jolt_attend_batch *batch, size_t *bytes);

@@ -1158,9 +1158,21 @@ PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype) {
     c.ws_bytes += (n + 255) / 256 * 256;
     return at;
   };
-  const size_t np = c.prefix_few ? (size_t)c.n_prefix * a.heads * rows : (size_t)c.n_prefix * a.n_tok * a.n_q;
-  const size_t nf = (size_t)c.few_items * a.heads * c.few_rows;
-  const size_t nm = (size_t)c.n_many * a.n_tok * a.n_q;
+  // Room for the most that the cut of this batch or of any smaller one takes (fewer requests, rows,
+  // rows of a request, tokens of prefix and tails), so that the size only grows with them, as those
+  // cuts need not: runs times rows of a head.
+  //   prefix, few():  n_prefix <= RUN_PREFIX-token runs, workgroups of a head; at most 32 rows.
+  //   prefix, many(): with of <= BLOCKS / heads workgroups and tiles >= rows / (64 nq),
+  //                   n_prefix < of / tiles + 2, and n_prefix <= kv_tiles.
+  //   tails, many():  n_many <= max(1, BLOCKS / (heads many_tiles)), many_tiles > rows / (64 many_nq).
+  const int64_t of = std::max(1, BLOCKS / a.heads);
+  int64_t most_prefix = 0, most_many = 0;
+  if (a.T > 0) {
+    most_prefix = std::min<int64_t>(ceil_div(a.T, RUN_PREFIX), of) * std::min<int64_t>(rows, 32);
+    if (rows > 32) most_prefix = std::max(most_prefix, std::min((int64_t)c.kv_tiles * rows, 128 * of + 2 * rows));
+  }
+  if (c.tails_many) most_many = std::max(rows, std::min<int64_t>(16 * rows, ceil_div(128 * BLOCKS, a.heads)));
+  const size_t np = (size_t)most_prefix * a.heads, nf = (size_t)c.few_items * c.few_rows * a.heads, nm = (size_t)most_many * a.heads;
   c.off_po = take(np * d * 4); c.off_pm = take(np * 8);
   c.off_fo = take(nf * d * 4); c.off_fm = take(nf * 8);
   c.off_mo = take(nm * d * 4); c.off_mm = take(nm * 8);

@@ -1,6 +1,8 @@
 """Host-side checks of the shared-prefix serving operators at the edges of what they accept (no GPU
-needed): tensors that do not hold what a descriptor reaches.
+needed): tensors that do not hold what a descriptor reaches, and workspaces of smaller batches.
 """
+import random
+
 import pytest
 import torch
 
@@ -75,3 +77,44 @@ def test_host_pools_prefix_and_workspace_never_reach_a_kernel():
         with pytest.raises(ValueError, match="n_req, max_pages"):
             J._marshal.columns(t, 3, "table")
     assert J._marshal.columns(ok["table"], 3, "table") == 2
+
+
+def _size(n_req, n_tok, max_new, T, max_pages, H, G, d, page, dtype):
+    pre = None if T == 0 else J.cell_desc(dtype=dtype, n_layers=1, n_heads=H, T=T, d=d, stride_layer=H * T * d, stride_head=T * d, stride_token=d)
+    pages = None if max_pages == 0 else J.page_desc(dtype=dtype, n_heads=H, page_size=page, d=d, n_pages=4, stride_page=H * page * d,
+                                                    stride_head=page * d, stride_token=d)
+    return J.jolt_prefix_attend_workspace_size(n_req, n_tok, H * G, prefix=pre, pages=pages, max_pages=max_pages, max_new=max_new)
+
+
+def test_a_smaller_batch_needs_no_larger_workspace():
+    """Along each size of a batch downwards, and from random batches to random smaller ones."""
+    model = dict(H=8, G=4, d=128, page=16, dtype=J.JOLT_BF16)
+    for base, axis, hi in ((dict(n_tok=256, max_new=1, T=4096, max_pages=40), "n_req", 256), (dict(n_req=64, max_new=0, T=4096, max_pages=40), "n_tok", 2100),
+                           (dict(n_req=64, n_tok=700, T=300, max_pages=40), "max_new", 700), (dict(n_req=3, n_tok=70, max_new=0, max_pages=0), "T", 9000),
+                           (dict(n_req=3, n_tok=9, max_new=1, max_pages=4), "T", 70000), (dict(n_req=9, n_tok=9, max_new=1, T=0), "max_pages", 50)):
+        last = 0
+        for x in range(1, hi + 1, 1 + hi // 2500):
+            kw = {**base, **model, axis: x}
+            if axis == "n_req":
+                kw["n_tok"] = x
+            n = _size(**kw)
+            assert n >= last, (axis, x)
+            last = n
+    rng = random.Random(0)
+
+    def log_int(hi):
+        return min(hi, int(2 ** rng.uniform(0, hi.bit_length())))
+    for _ in range(6000):
+        model = dict(H=rng.choice([1, 2, 3, 8, 40, 600]), G=rng.choice([1, 3, 4, 8]), d=rng.choice([32, 64, 128]), page=rng.choice([4, 64]),
+                     dtype=rng.choice([J.JOLT_BF16, J.JOLT_F32]))
+        top = dict(n_req=log_int(4096), n_tok=log_int(5000), max_new=log_int(600), T=rng.choice([0, log_int(40000)]), max_pages=log_int(300))
+        new = min(top["max_new"], top["n_tok"])
+        low = {k: max(1, log_int(v)) if v else 0 for k, v in top.items()}
+        low["max_new"] = log_int(new)
+        if rng.random() < 0.2:              # not given: as many as there are rows
+            top["max_new"] = low["max_new"] = 0
+        if rng.random() < 0.1:
+            low["max_pages"], low["T"] = rng.choice([(0, max(1, low["T"])), (low["max_pages"], 0)])
+            if low["T"] and not top["T"]:
+                continue
+        assert _size(**low, **model) <= _size(**top, **model), (low, top, model)
