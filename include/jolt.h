@@ -515,6 +515,15 @@ int jolt_prefix_attend(jolt_ctx *ctx, const jolt_cell_desc *prefix, const void *
                        const int32_t *kv_len, const void *Q, float scale, void *O, float *lse, void *ws,
                        size_t ws_bytes, jolt_stream stream);
 
+/* Test hook: how jolt_prefix_attend cuts a call of these sizes, so that a test can tell which
+ * kernels it runs: out[0] whether it is one launch, [1] rows of a row tile of the prefix (16 or 32:
+ * workgroups without shared tiles, 64 or 128: with; 0: no prefix), [2] most runs of a row of it,
+ * [3] row tiles of a head, [4] tiles of tokens and [5] pairs of both that a workgroup takes (64 and
+ * 128 rows only), [6] rows that a wave takes of tails of few rows, [7] rows of a row tile of those of
+ * many (0: none), [8] their runs, [9] lanes that join the runs of a row. */
+int jolt_debug_prefix_cut(const jolt_cell_desc *prefix, const jolt_page_desc *pages,
+                          const jolt_attend_batch *batch, int64_t *out);
+
 /* Test hook: copies an intermediate of the most recent jolt_compress on this
  * context for cell `cell` into dst (device memory, dst_bytes): 0 = U_T (T x r_T fp32),
  * 1 = U_d (d x r_d fp32), 2 = X~ (m x T x d fp32 from the stored factors, recomputed by

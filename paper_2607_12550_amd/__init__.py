@@ -25,7 +25,7 @@ __all__ = ["JoltError", "lib", "CellDesc", "SpectrumOpts", "Params", "CellSpectr
            "jolt_attend_workspace_size", "jolt_attend", "jolt_attend_noalloc", "JOLT_ATTEND_SCRATCH_BYTES", "jolt_debug_export", "jolt_debug_set",
            "PageDesc", "RowStrides", "AttendBatch", "page_desc", "jolt_page_plan", "jolt_page_append",
            "jolt_prefix_attend_workspace_size", "jolt_prefix_attend", "JOLT_PLAN_NO_PAGES", "JOLT_PLAN_TABLE_FULL",
-           "JOLT_PLAN_NO_TOKENS", "JOLT_PLAN_BAD_LENGTH",
+           "JOLT_PLAN_NO_TOKENS", "JOLT_PLAN_BAD_LENGTH", "jolt_debug_prefix_cut",
            "jolt_profile_enable", "jolt_profile_reset", "JOLT_E_NONFINITE", "JOLT_E_NOCONV",
            "JOLT_DBG_INVIT_ITERS", "JOLT_DBG_TRD_LANES", "JOLT_DBG_TRD_TWO_STAGE", "JOLT_DBG_BULGE_SPIN", "JOLT_DBG_TRD_GATHER",
            "jolt_profile_read", "STAGES", "cell_desc", "LIB_PATH", "HEADER_PATH"]
@@ -164,6 +164,7 @@ _SIGS = {
     "jolt_prefix_attend_workspace_size": (C.c_int, [_P(CellDesc), _P(PageDesc), _P(AttendBatch), _P(_sz)]),
     "jolt_prefix_attend": (C.c_int, [_vp, _P(CellDesc), _vp, _vp, C.c_int, _P(PageDesc), _vp, _vp, _vp,
                                      _P(AttendBatch), _vp, _vp, _vp, C.c_float, _vp, _vp, _vp, _sz, _vp]),
+    "jolt_debug_prefix_cut": (C.c_int, [_P(CellDesc), _P(PageDesc), _P(AttendBatch), _P(C.c_int64)]),
     "jolt_profile_enable": (C.c_int, [_vp, C.c_int]),
     "jolt_profile_reset": (C.c_int, [_vp]),
     "jolt_profile_read": (C.c_int, [_vp, C.c_int, _P(_dbl), _P(C.c_int64)]),
@@ -511,6 +512,15 @@ def jolt_prefix_attend_workspace_size(n_req: int, n_tok: int, n_q: int, prefix=N
     _check(lib.jolt_prefix_attend_workspace_size(None if prefix is None else C.byref(prefix),
                                                  None if pages is None else C.byref(pages), C.byref(b), C.byref(n)))
     return n.value
+
+
+def jolt_debug_prefix_cut(n_req: int, n_tok: int, n_q: int, prefix=None, pages=None, max_pages: int = 0, max_new: int = 0) -> dict:
+    """How jolt_prefix_attend cuts a call of these sizes (test hook)."""
+    d = pages.d if pages is not None else prefix.d
+    b, out = AttendBatch(n_req, n_tok, n_q, max_pages, max_new, 0, n_q * d, n_q * d), (C.c_int64 * 10)()
+    _check(lib.jolt_debug_prefix_cut(None if prefix is None else C.byref(prefix), None if pages is None else C.byref(pages), C.byref(b), out))
+    return dict(zip(("whole", "prefix_rows", "prefix_runs", "row_tiles", "token_tiles", "share", "few_rows", "many_rows", "many_runs",
+                     "join_lanes"), out))
 
 
 def jolt_prefix_attend(ctx, Q, O, q_start, kv_len, scale: float, ws, prefix=None, K_prefix=None, V_prefix=None,

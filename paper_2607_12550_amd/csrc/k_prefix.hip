@@ -1089,15 +1089,10 @@ hipError_t run(const PrefixAttendArgs &a, const PrefixCut &c, uint8_t *ws, hipSt
   p.n_few = (int)std::max<int64_t>(1, ceil_div((int64_t)c.few_items * a.heads, WAVES));
   k_runs<D, T><<<p.n_pre + p.n_many + p.n_few, NT, 0, st>>>(p);
   const JoinArgs j{a, pp, pf, pm, entries, c.n_prefix, c.prefix_few, 64 * c.prefix_nq, c.kv_tiles, c.share, c.few_rows, a.n_tok * a.group, c.few_items, c.n_many};
-  // A workgroup a row, a wave a row or D / 4 lanes a row: as many lanes as fill the chip, since the
-  // chain of reads bounds a row and the lanes that join at its end lengthen it (8192 rows of 10
-  // runs: 11 us by D / 4 lanes, 14 by waves; 2048 rows of 11: 7.3 and 6.0; 384 rows of 171: 9 us by
-  // waves, 6 by workgroups).
-  const int64_t out_rows = (int64_t)a.n_tok * a.n_q;
-  auto grid = [&](int lanes) { return grid_of(ceil_div(out_rows * lanes, NT)); };
-  if (out_rows <= 2 * BLOCKS) k_join<D, T, 64, true><<<grid(NT), NT, 0, st>>>(j);
-  else if (out_rows <= 8 * BLOCKS) k_join<D, T, 64, false><<<grid(64), NT, 0, st>>>(j);
-  else k_join<D, T, D / 4, false><<<grid(D / 4), NT, 0, st>>>(j);
+  const dim3 grid = grid_of(ceil_div((int64_t)a.n_tok * a.n_q * c.join_lanes, NT));
+  if (c.join_lanes == NT) k_join<D, T, 64, true><<<grid, NT, 0, st>>>(j);
+  else if (c.join_lanes == 64) k_join<D, T, 64, false><<<grid, NT, 0, st>>>(j);
+  else k_join<D, T, D / 4, false><<<grid, NT, 0, st>>>(j);
   return hipGetLastError();
 }
 
@@ -1135,6 +1130,12 @@ PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype) {
       cut_prefix(c, a, d, dtype == JOLT_BF16);
     }
   }
+  // A workgroup a row, a wave a row or D / 4 lanes a row: as many lanes as fill the chip, since the
+  // chain of reads bounds a row and the lanes that join at its end lengthen it (8192 rows of 10
+  // runs: 11 us by D / 4 lanes, 14 by waves; 2048 rows of 11: 7.3 and 6.0; 384 rows of 171: 9 us by
+  // waves, 6 by workgroups).
+  const int64_t out_rows = (int64_t)a.n_tok * a.n_q;
+  c.join_lanes = out_rows <= 2 * BLOCKS ? NT : out_rows <= 8 * BLOCKS ? 64 : d / 4;
   // without tails every request is one of few rows and no runs
   c.limit = 0x7fffffff;
   if (a.max_pages > 0) {

@@ -287,6 +287,7 @@ struct PrefixCut {
   int64_t share = 1;                                             // and (row tile, tile of tokens) pairs of each
   int32_t few_nq = 1, few_items = 0, few_rows = 0, limit = 0;    // tails of few rows
   int32_t many_nq = 1, many_tiles = 0, n_many = 0;               // and of many
+  int32_t join_lanes = 0;                                        // of a row and query head
   size_t off_po = 0, off_pm = 0, off_fo = 0, off_fm = 0, off_mo = 0, off_mm = 0, off_entries = 0, ws_bytes = 0;
 };
 PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype);

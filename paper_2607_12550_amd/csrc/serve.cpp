@@ -185,6 +185,28 @@ extern "C" int jolt_prefix_attend_workspace_size(const jolt_cell_desc *prefix, c
   return JOLT_OK;
 }
 
+extern "C" int jolt_debug_prefix_cut(const jolt_cell_desc *prefix, const jolt_page_desc *pages,
+                                     const jolt_attend_batch *batch, int64_t *out) {
+  PrefixAttendArgs a;
+  int d, dtype;
+  int rc = resolve_prefix_attend(prefix, pages, batch, &a, &d, &dtype);
+  if (rc) return rc;
+  if (!out) return jolt_fail(JOLT_E_INVAL, "jolt_debug_prefix_cut: out is null");
+  const PrefixCut c = prefix_attend_cut(a, d, dtype);
+  const bool pre = a.T > 0 && !c.whole, tails = a.max_pages > 0 && !c.whole;
+  out[0] = c.whole;
+  out[1] = !pre ? 0 : (c.prefix_few ? 16 : 64) * c.prefix_nq;
+  out[2] = c.n_prefix;
+  out[3] = pre && !c.prefix_few ? c.prefix_tiles : 0;
+  out[4] = pre && !c.prefix_few ? c.kv_tiles : 0;
+  out[5] = pre && !c.prefix_few ? c.share : 0;
+  out[6] = tails || c.whole ? 16 * c.few_nq : 0;
+  out[7] = tails && c.tails_many ? 64 * c.many_nq : 0;
+  out[8] = c.n_many;
+  out[9] = c.join_lanes;
+  return JOLT_OK;
+}
+
 extern "C" int jolt_prefix_attend(jolt_ctx *ctx, const jolt_cell_desc *prefix, const void *K, const void *V, int layer,
                                   const jolt_page_desc *pages, const void *K_pages, const void *V_pages,
                                   const int32_t *table, const jolt_attend_batch *batch, const int32_t *q_start,

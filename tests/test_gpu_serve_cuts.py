@@ -1,0 +1,90 @@
+"""GPU tests of jolt_prefix_attend over calls that run each of its kernels' forms (serve_cuts.py):
+random inputs against the definition in float64, with the tolerances of test_gpu_serve.py, and
+equal weights over values of which every one counts.
+"""
+import numpy as np
+import pytest
+import torch
+
+from serve_cuts import CUTS, cut, name
+from test_gpu_serve import CASES, DT, Batch
+
+pytestmark = pytest.mark.gpu
+
+
+def want64(b):
+    """What b.want() gives, request by request in float64 on the GPU."""
+    H, G, d = b.H, b.G, b.d
+    n_all = b.Q.shape[0]
+    O, A = (torch.full((n_all, H * G, d), float("nan"), dtype=torch.float64, device="cuda") for _ in range(2))
+    lse, S = (torch.full((n_all, H * G), float("nan"), dtype=torch.float64, device="cuda") for _ in range(2))
+    for r, length in enumerate(b.kv_len):
+        q0, q1 = int(b.q_start[r]), int(b.q_start[r + 1])
+        n = q1 - q0
+        if n == 0:
+            continue
+        k, v = (torch.cat(([x[1][:, :b.T]] if b.T else []) + [t[r][:, :length]], 1).double() for x, t in ((b.K, b.tk), (b.V, b.tv)))
+        q = b.Q[q0:q1].double().reshape(n, H, G, d).permute(1, 0, 2, 3).reshape(H, n * G, d)
+        kt = k.transpose(1, 2).contiguous()
+        hidden = torch.arange(k.shape[1], device="cuda") > (b.T + int(length) - n + torch.arange(n, device="cuda"))[:, None]
+        hidden = hidden.repeat_interleave(G, 0)
+        s = (b.scale * (q @ kt)).masked_fill(hidden, -np.inf)
+        top = s.amax(-1, keepdim=True)
+        p = (s - top).exp()
+        total = p.sum(-1, keepdim=True)
+
+        def put(dst, x):
+            dst[q0:q1] = x.reshape(H, n, G, *x.shape[2:]).transpose(0, 1).reshape(n, H * G, *x.shape[2:])
+        put(O, p @ v / total)
+        put(A, p @ v.abs() / total)
+        put(lse, (top + total.log())[..., 0])
+        put(S, (b.scale * (q.abs() @ kt.abs())).masked_fill(hidden, 0).amax(-1))
+    return tuple(x.cpu().numpy() for x in (O, lse, A, S))
+
+
+def test_the_definition_on_the_gpu_is_the_oracle():
+    b = Batch("bf16", 33, [5, 0, 40], [1, 9, 3], 2, 3, 32, 8, pad_rows=2)
+    for x, y in zip(want64(b), b.want()):
+        np.testing.assert_allclose(x, y, rtol=1e-10, atol=1e-12)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("call,rows,how,many,join", CUTS, ids=[name(c[0]) for c in CUTS])
+def test_every_form_of_the_kernels(dtype, call, rows, how, many, join):
+    b = Batch(dtype, *call, seed=call[0])
+    assert cut(dtype, call)["prefix_rows"] == rows[dtype != "bf16"]
+    b.check(b.run(max_new=max(call[2])), want64(b))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("call", [c[0] for c in CUTS] + CASES, ids=name)
+def test_every_token_counts(dtype, call):
+    """Queries of zero weigh all tokens alike, 2^-8 or its product with a power of two, and token x
+    has the value 1 at feature (x + 5 h) % d and 0 elsewhere: sums are whole multiples of the weight
+    and exact, so that an output is off by the rounding of 1 / l, of its product and of itself (half a
+    step), and a token that is lost or taken twice moves one by far more.  lse is ln of the
+    number of tokens: log2 right to two steps of a value below 16, two roundings of sums
+    below 32 and one product, in all below 2^-18."""
+    T, have, new, H, G, d, page = call
+    b = Batch(dtype, *call)
+    b.Q.zero_()
+    eye = torch.eye(d, device="cuda", dtype=b.V.dtype)
+    heads = 5 * torch.arange(H, device="cuda")[:, None]
+    b.V[1] = eye[(torch.arange(b.V.shape[2], device="cuda") + heads) % d]
+    at = torch.arange(int(b.kv_len.max()), device="cuda")
+    tail = eye[(at + 3 + heads) % d]                                        # [H][tokens][d]
+    columns = torch.as_tensor(b.table, device="cuda").clamp(min=0).long()
+    for r, length in enumerate(b.kv_len):
+        x = at[:int(length)]
+        b.Vp[columns[r, x // page], :, x % page] = tail[:, :int(length)].transpose(0, 1)
+    O, lse = b.run(max_new=max(new))
+    pre = b.V[1][:, :T].double().sum(1)
+    running = torch.cat([torch.zeros((H, 1, d), dtype=torch.float64, device="cuda"), tail.double().cumsum(1)], 1)
+    tol = DT[dtype][2] + 2.0 ** -22
+    for r, length in enumerate(b.kv_len):
+        q0, n = int(b.q_start[r]), int(b.q_start[r + 1] - b.q_start[r])
+        seen = (int(length) - n + 1 + torch.arange(n, device="cuda")).clamp(min=0)
+        count = (T + seen).double()[:, None, None]
+        want = ((pre + running[:, seen].transpose(0, 1)) / count).repeat_interleave(G, 1).cpu().numpy()
+        assert (np.abs(O[q0:q0 + n] - want) <= tol * want).all(), r
+        assert (np.abs(lse[q0:q0 + n] - count.log()[..., 0].cpu().numpy()) <= 2.0 ** -18).all(), r

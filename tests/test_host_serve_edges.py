@@ -1,5 +1,6 @@
 """Host-side checks of the shared-prefix serving operators at the edges of what they accept (no GPU
-needed): tensors that do not hold what a descriptor reaches, and workspaces of smaller batches.
+needed): tensors that do not hold what a descriptor reaches, workspaces of smaller batches, and the
+choice of kernels that the GPU tests rely on.
 """
 import random
 
@@ -7,6 +8,7 @@ import pytest
 import torch
 
 import paper_2607_12550_amd as J
+from serve_cuts import CUTS, cut
 from test_host_serve import A, _pages, _prefix
 
 
@@ -118,3 +120,26 @@ def test_a_smaller_batch_needs_no_larger_workspace():
             if low["T"] and not top["T"]:
                 continue
         assert _size(**low, **model) <= _size(**top, **model), (low, top, model)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_calls_run_the_kernels_that_they_are_meant_to_test(dtype):
+    """Each call's form, and that the calls together reach every one of both types."""
+    seen = set()
+    for call, rows, how, many, join in CUTS:
+        c, d = cut(dtype, call), call[5]
+        assert not c["whole"] and c["prefix_rows"] == rows[dtype != "bf16"] and c["many_rows"] == many and c["join_lanes"] == join
+        assert (c["share"] > c["token_tiles"]) == (how == "several") and c["prefix_runs"] > 1
+        assert call[0] % (64 if dtype == "bf16" else 32)                     # the last tile of tokens is not full
+        seen |= {("prefix", d, c["prefix_rows"]), ("join", d, join), ("long tails", many), ("ends in a row tile", c["token_tiles"] % c["share"] != 0), how}
+    assert {("prefix", 64, 64), ("prefix", 64, 128), ("prefix", 128, 64), ("prefix", 128, 128), ("join", 32, 8), ("join", 64, 16), ("join", 128, 32),
+            ("join", 128, 64), ("join", 64, 256), ("long tails", 64), ("long tails", 128), ("ends in a row tile", True), "several"} <= seen
+    small = cut(dtype, (60, [3, 7], [1, 1], 4, 2, 64, 16))
+    few = cut(dtype, (4001, [9] * 17, [1] * 17, 40, 1, 128, 16))
+    assert small["whole"] and few["prefix_rows"] == 32 and not few["whole"]
+
+
+def test_the_cut_refuses_what_the_call_refuses():
+    with pytest.raises(J.JoltError, match="multiple"):
+        J.jolt_debug_prefix_cut(4, 8, 12, pages=_pages(), max_pages=3)
+    assert J.lib.jolt_debug_prefix_cut(None, None, None, None) == J.JOLT_E_INVAL
