@@ -5,7 +5,8 @@ kernels.  Functions keep the C-ABI names (``jolt_spectrum``, ``jolt_compress``,
 ``jolt_decompress``, ``jolt_allocate`` ...).  Device buffers are passed as torch
 CUDA tensors (or raw integer device addresses); streams as ``torch.cuda.Stream``
 or raw ``hipStream_t`` integers.  If the compiled library is missing, importing
-this package raises: there is no fallback implementation.
+this package raises, and without ``_marshal.so`` the serving calls do: there is no
+fallback implementation.
 """
 from __future__ import annotations
 
@@ -65,7 +66,23 @@ if not os.path.exists(LIB_PATH):
 import torch  # noqa: E402,F401
 
 lib = C.CDLL(LIB_PATH)
-from . import _marshal  # noqa: E402
+
+
+class _MissingMarshal:
+    """In the place of a ``_marshal.so`` that does not load: only the serving calls need it."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"the serving calls (jolt_page_plan, jolt_page_append, jolt_prefix_attend) need {HERE}/_marshal.so ({self._why}): "
+                          "build it with `python paper_2607_12550_amd/build.py` (or __graft_entry__.build())")
+
+
+try:
+    from . import _marshal  # noqa: E402
+except ImportError as e:
+    _marshal = _MissingMarshal(e)
 
 
 class CellDesc(C.Structure):

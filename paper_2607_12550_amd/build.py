@@ -4,7 +4,8 @@ Usage: ``python -m paper_2607_12550_amd.build`` (or ``build()`` from Python).
 Every HIP source is compiled for gfx950 only; host-only sources are compiled
 without floating-point contraction so the allocator's double arithmetic is
 plain IEEE.  Objects go to ``_build/`` next to this file.  ``_marshal.so`` is the Python binding's check of
-tensor arguments, against torch's own headers and library.
+the serving calls' tensors, built by g++ against torch's own headers and library; the library is in place
+also where that fails.
 """
 from __future__ import annotations
 
@@ -66,13 +67,13 @@ def build(verbose: bool = False) -> str:
     with ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
         marshal = ex.submit(_marshal)
         objs = list(ex.map(lambda j: _compile(*j), jobs))
-        marshal.result()
     tmp = OUT + ".tmp"
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stdout + r.stderr)
     os.replace(tmp, OUT)
+    marshal.result()       # after the library: only the serving calls of the binding need it
     if verbose:
         print("built", OUT)
     return OUT

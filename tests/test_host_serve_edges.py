@@ -1,8 +1,12 @@
 """Host-side checks of the shared-prefix serving operators at the edges of what they accept (no GPU
 needed): tensors that do not hold what a descriptor reaches, workspaces of smaller batches, and the
-choice of kernels that the GPU tests rely on.
+choice of kernels that the GPU tests rely on; and a package without the binding's native checks.
 """
+import os
 import random
+import subprocess
+import sys
+import types
 
 import pytest
 import torch
@@ -143,3 +147,45 @@ def test_the_cut_refuses_what_the_call_refuses():
     with pytest.raises(J.JoltError, match="multiple"):
         J.jolt_debug_prefix_cut(4, 8, 12, pages=_pages(), max_pages=3)
     assert J.lib.jolt_debug_prefix_cut(None, None, None, None) == J.JOLT_E_INVAL
+
+
+def test_without_the_native_checks_only_the_serving_calls_are_gone():
+    code = """
+import sys
+sys.modules["paper_2607_12550_amd._marshal"] = None           # an import of it fails
+import paper_2607_12550_amd as J
+assert J.jolt_q_cap(4096, 4.0) > 0
+import torch
+z = torch.zeros(4, dtype=torch.int32)
+pages = J.page_desc(dtype=J.JOLT_BF16, n_heads=1, page_size=8, d=32, n_pages=1, stride_page=256, stride_head=256, stride_token=32)
+for call in (lambda: J.jolt_page_plan(None, pages, *[z] * 11), lambda: J.jolt_page_append(None, pages, z, z, z, z, z),
+             lambda: J.jolt_prefix_attend(None, z, z, z, z, 0.1, z, pages=pages)):
+    try:
+        call()
+    except ImportError as e:
+        assert "_marshal.so" in str(e) and "build" in str(e), e
+    else:
+        raise SystemExit("no error")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_the_library_is_built_where_the_native_checks_are_not(monkeypatch, tmp_path):
+    from paper_2607_12550_amd import build as B
+
+    def no_compiler():
+        raise RuntimeError("no g++")
+
+    def link(cmd, **kw):
+        open(cmd[cmd.index("-o") + 1], "w").close()
+        return types.SimpleNamespace(returncode=0, stdout="", stderr="")
+    monkeypatch.setattr(B, "_compile", lambda src, extra: src)
+    monkeypatch.setattr(B, "_marshal", no_compiler)
+    monkeypatch.setattr(B, "BUILD", str(tmp_path / "objects"))
+    monkeypatch.setattr(B, "OUT", str(tmp_path / "lib.so"))
+    monkeypatch.setattr(B, "subprocess", types.SimpleNamespace(run=link))
+    with pytest.raises(RuntimeError, match="no g"):
+        B.build()
+    assert (tmp_path / "lib.so").exists()
