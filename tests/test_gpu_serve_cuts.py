@@ -88,3 +88,28 @@ def test_every_token_counts(dtype, call):
         want = ((pre + running[:, seen].transpose(0, 1)) / count).repeat_interleave(G, 1).cpu().numpy()
         assert (np.abs(O[q0:q0 + n] - want) <= tol * want).all(), r
         assert (np.abs(lse[q0:q0 + n] - count.log()[..., 0].cpu().numpy()) <= 2.0 ** -18).all(), r
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_heads_than_workgroups_fill_the_chip(dtype):
+    for call in ((70, [5, 3], [1, 2], 1024, 1, 32, 8), (300, [500, 0, 2], [1, 2, 1], 600, 2, 64, 16), (200, [3, 40], [40, 2], 513, 1, 64, 16)):
+        b = Batch(dtype, *call)
+        b.check(b.run(max_new=max(call[2])), want64(b))
+
+
+@pytest.mark.parametrize("new,T", [([1, 1, 2], 40), ([1, 3, 2], 900), ([40, 1, 9], 300)])
+def test_rows_before_the_first_request_are_left(new, T):
+    b = Batch("bf16", T, [9, 0, 50], new, 2, 4, 64, 8, pad_rows=11)
+    b.q_start = b.q_start + 7
+    b.check(b.run(max_new=max(new)), want64(b))
+
+
+@pytest.mark.parametrize("new,T", [([1, 1, 2], 40), ([1, 3, 2], 900), ([40, 1, 9], 300)])
+def test_requests_that_share_pages(new, T):
+    """One tail's pages in the tables of two requests, and a page twice in one table."""
+    b = Batch("bf16", T, [30, 30 + new[0] - new[1], 70], new, 2, 4, 64, 8)
+    b.table[1], b.tk[1], b.tv[1] = b.table[0], b.tk[0], b.tv[0]
+    b.table[2, 3] = b.table[2, 1]
+    for x in (b.tk, b.tv):
+        x[2][:, 24:32] = x[2][:, 8:16]
+    b.check(b.run(max_new=max(new)), want64(b))
