@@ -474,7 +474,8 @@ typedef struct {
   int32_t n_q;             /* query heads, a multiple G of the key-value heads; G <= 64 */
   int32_t max_pages;       /* columns of the table */
   int32_t max_new;         /* most rows of one request; 0: not known (n_tok is then taken).  It
-                              picks the kernels; a request with more rows counts as having none */
+                              picks the kernels; a request with more rows counts as having none,
+                              and its rows of O and lse keep what they held */
   int32_t reserved;
   int64_t q_stride, o_stride; /* elements between rows of Q and O (multiples of 8, >= n_q * d) */
 } jolt_attend_batch;
@@ -485,7 +486,8 @@ typedef struct {
  * j / (n_q / n_heads).  Row t attends to all T tokens of the prefix and to the first
  * kv_len[r] - n + i + 1 tokens of the tail (none where that is below 1):
  *   O[t][j] = sum_x softmax_x(scale * Q[t][j] . k_x) v_x,
- *   lse[t][j] = ln sum_x exp(scale * Q[t][j] . k_x)   (fp32, [n_tok][n_q]; may be NULL).
+ *   lse[t][j] = ln sum_x exp(scale * Q[t][j] . k_x)   (fp32, [n_tok][n_q]; may be NULL),
+ * with 0 < scale < 2^127.
  * A row that attends to nothing gets O = 0 and lse = -inf.  What a row does not attend to has
  * no part in its result, NaN and infinities included.  Rows t of no request are left as they
  * were.  The keys and values of the prefix are read once for all rows that fit a tile

@@ -226,7 +226,8 @@ extern "C" int jolt_prefix_attend(jolt_ctx *ctx, const jolt_cell_desc *prefix, c
       (pages && (misaligned(K_pages, 16) || misaligned(V_pages, 16))))
     return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: Q, O, keys and values must be 16-byte aligned");
   if (misaligned(ws, 256)) return jolt_fail(JOLT_E_INVAL, "workspace must be 256-byte aligned");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: scale must be > 0");
+  // the kernels form scores in units of log2: scale * log2(e) has to be finite too
+  if (!(scale > 0.f) || !(scale < 0x1p127f)) return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: scale must be > 0 and below 2^127");
   const PrefixCut cut = prefix_attend_cut(a, d, dtype);
   if (ws_bytes < cut.ws_bytes) return jolt_fail(JOLT_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, cut.ws_bytes);
   if (!ctx) return jolt_fail(JOLT_E_INVAL, "jolt_prefix_attend: ctx is null");

@@ -13,7 +13,7 @@ import torch
 
 import paper_2607_12550_amd as J
 from serve_cuts import CUTS, cut
-from test_host_serve import A, _pages, _prefix
+from test_host_serve import A, _attend, _pages, _prefix, _refused
 
 
 def _small(**kw):
@@ -189,3 +189,10 @@ def test_the_library_is_built_where_the_native_checks_are_not(monkeypatch, tmp_p
     with pytest.raises(RuntimeError, match="no g"):
         B.build()
     assert (tmp_path / "lib.so").exists()
+
+
+def test_scales_whose_scores_in_units_of_log2_overflow_are_refused():
+    for scale in (2.0 ** 127, 3e38):
+        _refused(_attend(scale=scale), J.JOLT_E_INVAL, "scale")
+    for scale in (1e38, 1e-45):
+        _refused(_attend(scale=scale), J.JOLT_E_INVAL, "ctx is null")
