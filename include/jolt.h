@@ -472,7 +472,10 @@ typedef struct {
   int32_t n_req;           /* requests (1..4096) */
   int32_t n_tok;           /* packed rows of Q and O (>= 1) */
   int32_t n_q;             /* query heads, a multiple G of the key-value heads; G <= 64 */
-  int32_t max_pages;       /* columns of the table */
+  int32_t max_pages;       /* columns of the table.  Their room picks the kernels, whatever requests
+                              hold: calls of up to 32 rows a request and key-value head, up to 384
+                              tokens (fp32 192) of prefix and room, and few requests times heads
+                              are one launch, others two */
   int32_t max_new;         /* most rows of one request; 0: not known (n_tok is then taken).  It
                               picks the kernels; a request with more rows counts as having none,
                               and its rows of O and lse keep what they held */
@@ -491,7 +494,7 @@ typedef struct {
  * A row that attends to nothing gets O = 0 and lse = -inf.  What a row does not attend to has
  * no part in its result, NaN and infinities included.  Rows t of no request are left as they
  * were.  The keys and values of the prefix are read once for all rows that fit a tile
- * together, not once per request.
+ * together, not once per request (once per request by the short calls named at max_pages).
  *   prefix     layer `layer` of a cell with keys K and values V (one descriptor for both);
  *              NULL: no prefix.  T < 2^20.
  *   pages      K_pages, V_pages and table [n_req][max_pages] of the tails; NULL: no tails

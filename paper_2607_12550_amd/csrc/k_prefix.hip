@@ -291,8 +291,10 @@ struct Rows {
     }
   }
   // o += V^T P^T for 16 SUBS tokens whose values stand in LDS; the weights are
-  // rounded to bf16 for the bf16 product (values are bf16 already): half a step each, which
-  // averages out over the tokens, for half of the matrix work of two terms.
+  // rounded to bf16 for the bf16 product (values are bf16 already): half a step each, which averages
+  // out over the tokens (the output's error grows to 1.2 .. 1.4 times that of its own rounding), for
+  // half of the matrix work of two terms: those take 225 us for 256 requests on 32768 tokens, not
+  // 195, and 132 for 1025 prompt rows on 4096, not 115.
   template <int SUBS>
   JOLT_DEV void values(const f4_t (&p)[SUBS][NQ], const uint8_t *v, int n16, int g) {
     if constexpr (G::BF) {
