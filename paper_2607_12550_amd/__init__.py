@@ -507,7 +507,7 @@ def jolt_page_plan(ctx, pages: PageDesc, have, add, free_pages, n_free, table, k
 def jolt_page_append(ctx, pages: PageDesc, K, V, slots, K_pages, V_pages, positions=None, rope=None, stream=None) -> None:
     """Writes the rows K, V [n_tok, n_heads, d] into their slots of the pools; rope: None, or
     (base, position_offset) to rotate the keys at positions + position_offset.  The pools are tensors of the
-    descriptor's type whose memory holds all of its pages, or addresses."""
+    descriptor's type, or of bytes, whose memory holds all of its pages, or addresses."""
     n, bf16, heads, d = slots.numel(), pages.dtype == JOLT_BF16, pages.n_heads, pages.d
     if n > _INT_MAX:
         raise ValueError("slots hold at most 2^31 - 1 elements")
@@ -547,7 +547,7 @@ def jolt_prefix_attend(ctx, Q, O, q_start, kv_len, scale: float, ws, prefix=None
     share (layer `layer` of the cell `prefix`) and each request's own pages; writes O and, if
     given, lse [n_tok, n_q] fp32.  q_start [n_req + 1], kv_len [n_req], table [n_req, max_pages]
     are device int32 tensors.  Cell, pools and workspace are tensors whose memory holds what their
-    descriptors (ws: ws_bytes, or its own size) reach, of the descriptors' type, or addresses."""
+    descriptors (ws: ws_bytes, or its own size) reach, of the descriptors' type or of bytes, or addresses."""
     n_req = q_start.numel() - 1
     desc = pages if pages is not None else prefix
     if desc is None:

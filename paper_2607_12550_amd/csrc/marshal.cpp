@@ -90,8 +90,8 @@ PyObject *rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 // The address of memory for `need` elements of `type` (nullptr: bytes, of any type): None is 0, a
-// whole number an address that the caller answers for, a tensor one whose storage reaches that far
-// from its first element.  Returns false with an error set.
+// whole number an address that the caller answers for, a tensor one of that type, or of plain bytes,
+// whose storage reaches that far from its first element.  Returns false with an error set.
 bool memory(PyObject *o, const at::ScalarType *type, __int128 need, const char *name, PyObject *&out) {
   if (o == Py_None) return (out = PyLong_FromLong(0)) != nullptr;
   if (PyLong_Check(o)) {
@@ -101,12 +101,12 @@ bool memory(PyObject *o, const at::ScalarType *type, __int128 need, const char *
   }
   const at::Tensor *t = tensor(o, name);
   if (!t) return false;
-  if (type && t->scalar_type() != *type) {
+  if (type && t->scalar_type() != *type && t->scalar_type() != at::kByte) {
     PyErr_Format(PyExc_ValueError, "%s must be a %s tensor", name, *type == at::kBFloat16 ? "bfloat16" : "float32");
     return false;
   }
-  const __int128 size = t->element_size();
-  if (((__int128)t->storage().nbytes() - (__int128)t->storage_offset() * size) / (type ? size : 1) < need) {
+  const __int128 held = (__int128)t->storage().nbytes() - (__int128)t->storage_offset() * t->element_size();
+  if (held / (type ? (int)at::elementSize(*type) : 1) < need) {
     PyErr_Format(PyExc_ValueError, "%s: the call reaches %lld %s, more than the tensor's memory holds from its first element on", name,
                  (long long)need, type ? "elements" : "bytes");
     return false;

@@ -35,7 +35,7 @@ def test_memory_that_a_descriptor_reaches_is_checked():
     one that fits in all else shows that."""
     big = torch.zeros(1000, dtype=torch.bfloat16)
     for bad, word in ((_t(768, torch.float32), "bfloat16"), (_t(767), "768 elements"), (big[300:], "768 elements"),
-                      (_t(1).expand(768), "768 elements"), (_t(768), "on the GPU"), (big[232:], "on the GPU"), ([1], "must be a tensor")):
+                      (_t(1).expand(768), "768 elements"), (_t(1535, torch.uint8), "768 elements"), (_t(1536, torch.uint8), "on the GPU"), (_t(768), "on the GPU"), (big[232:], "on the GPU"), ([1], "must be a tensor")):
         for K, V, name in ((bad, A, "K_pages"), (A, bad, "V_pages")):
             with pytest.raises(ValueError, match=name) as e:
                 J._marshal.pools(_small(), K, V)
