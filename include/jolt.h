@@ -502,8 +502,8 @@ typedef struct {
  *              max_pages * page_size (< 2^30); tokens of a page index outside
  *              0..n_pages - 1 are not attended to.
  * Q, O ([n_tok][n_q][d]), prefix and pages are of one type.  bf16: the products are of bf16
- * values summed in fp32, scores and softmax in fp32, the softmax weights rounded to bf16 for
- * the value product, O rounded once.  fp32: fp32 throughout.  Where the sum of |v_x| over the
+ * values summed in fp32, scores and softmax in fp32, the softmax weights two bf16 terms each in
+ * the value product (right to 2^-15), O rounded once.  fp32: fp32 throughout.  Where the sum of |v_x| over the
  * tokens that a row attends to is within fp32, O is finite.  Results do not depend on the
  * order of arrival of anything (no atomics): equal calls give equal bits.
  * O and lse overlap no input.  At most 1024 key-value heads, n_tok * n_q < 2^28.  ws: device,

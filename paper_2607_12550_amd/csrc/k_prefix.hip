@@ -290,22 +290,32 @@ struct Rows {
       for (int u = 0; u < SUBS; ++u) s[u][x] = p[u][x];
     }
   }
-  // o += V^T P^T for 16 SUBS tokens whose values stand in LDS; the weights are
-  // rounded to bf16 for the bf16 product (values are bf16 already): half a step each, which averages
-  // out over the tokens (the output's error grows to 1.2 .. 1.4 times that of its own rounding), for
-  // half of the matrix work of two terms: those take 225 us for 256 requests on 32768 tokens, not
-  // 195, and 132 for 1025 prompt rows on 4096, not 115.
+  // o += V^T P^T for 16 SUBS tokens whose values stand in LDS.  For the bf16 product (values are
+  // bf16 already) a weight is the sum of two bf16 terms, its upper half and the rest, right to 2^-15: the
+  // output's error is that of its own rounding.  One term, the weight rounded, makes it 1.2 .. 1.4
+  // times that, and takes 196 us for 256 requests on 32768 tokens, not 228, and 115 for 1025 prompt
+  // rows on 4096, not 135; calls that memory bounds take the same (64 requests on 4096 tokens 24.3 us).
+  // ABOVE_ONE adds 2^-23 of the weight to the rest, so that it is above zero wherever the weight is and
+  // times an infinite value no NaN.
+  static constexpr float ABOVE_ONE = 1.f + 0x1p-23f;
   template <int SUBS>
   JOLT_DEV void values(const f4_t (&p)[SUBS][NQ], const uint8_t *v, int n16, int g) {
     if constexpr (G::BF) {
 #pragma unroll
       for (int u = 0; u < SUBS; u += 2) {
-        b8_t w[NQ];
+        b8_t w[NQ], rest[NQ];
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
-          const uint32_t d[4] = {pack_bf16(p[u][x][0], p[u][x][1]), pack_bf16(p[u][x][2], p[u][x][3]),
-                                 pack_bf16(p[u + 1][x][0], p[u + 1][x][1]), pack_bf16(p[u + 1][x][2], p[u + 1][x][3])};
+          uint32_t d[4], r[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float y = p[u + i / 2][x][2 * (i % 2)], z = p[u + i / 2][x][2 * (i % 2) + 1];
+            const uint32_t yb = __float_as_uint(y), zb = __float_as_uint(z);
+            d[i] = __builtin_amdgcn_perm(zb, yb, 0x07060302u);   // the upper halves
+            r[i] = pack_bf16(fmaf(y, ABOVE_ONE, -__uint_as_float(yb & 0xffff0000u)), fmaf(z, ABOVE_ONE, -__uint_as_float(zb & 0xffff0000u)));
+          }
           __builtin_memcpy(&w[x], d, 16);
+          __builtin_memcpy(&rest[x], r, 16);
         }
         const uint8_t *base = v + (4 * g + (n16 >> 2)) * G::VP + 8 * (n16 & 3);
 #pragma unroll
@@ -319,6 +329,8 @@ struct Rows {
           __builtin_memcpy(&va, &xv, 16);
 #pragma unroll
           for (int x = 0; x < NQ; ++x) o[f][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, w[x], o[f][x], 0, 0, 0);
+#pragma unroll
+          for (int x = 0; x < NQ; ++x) o[f][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, rest[x], o[f][x], 0, 0, 0);
         }
       }
     } else {
@@ -1029,8 +1041,8 @@ int64_t ceil_div(int64_t x, int64_t y) { return (x + y - 1) / y; }
 // work, and a part that waits for memory and LDS) and 4 us to start and end a row tile; two on a
 // CU take 1.5 times as long as one; every run's output is written and read once more, at about
 // 4 MB a us and 0.1 us a run of a row.  Measured against it (prefix alone, us): 256 rows a head on
-// 4096 tokens, 64-row tiles in 4, 8, 16 and 32 runs 32, 22, 22 and 27, 128-row tiles 41, 27, 23 and
-// 25; 1024 rows on 32768 tokens, 8 runs 251 and 192.
+// 4096 tokens, 64-row tiles in 4, 8 and 16 runs 29, 20 and 20, 128-row tiles in 8, 16 and 32 runs 25,
+// 21 and 25; 1024 rows on 32768 tokens by 64 workgroups a head 243 and 193.
 void cut_prefix(PrefixCut &c, const PrefixAttendArgs &a, int d, bool bf16) {
   const int64_t rows = (int64_t)a.n_tok * a.group, tokens = bf16 ? 64 : 32;
   const double out = (double)a.n_tok * a.n_q * d * 8 / 4e6;
@@ -1108,9 +1120,9 @@ PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype) {
   // all of a request and head to one workgroup: for those of few rows and up to 3 steps of its
   // waves (128 tokens each, fp32 64), at most 4 steps counted once for every 256 workgroups.  In one
   // launch and in two (us; d 128, bf16 and fp32):
-  //     32 workgroups, 3 steps  9.7 and 11.3, 11.5 and 13.8;  4 steps 11.7 and 11.4, 14.0 and 14.0
-  //    512 workgroups, 2 steps 11.4 and 13.6, 14.1 and 16.1;  3 steps 15.7 and 15.3, (4) 20.2 and 18.6
-  //   1024 workgroups, 1 step  14.7 and 15.8, 15.1 and 17.0;  2 steps 21.4 and 17.1, 25.7 and 20.9
+  //     32 workgroups, 3 steps 10.6 and 12.3, 11.1 and 13.8;  4 steps 12.8 and 12.8, 13.4 and 14.1
+  //    512 workgroups, 2 steps 13.1 and 13.5, 13.3 and 13.2;  3 steps 16.2 and 13.2, 17.5 and 16.1
+  //   1024 workgroups, 1 step  16.2 and 16.6, 15.2 and 17.1;  2 steps 23.2 and 15.8, 24.3 and 18.0
   const int64_t steps = ceil_div(a.T + ((int64_t)a.max_pages << a.tail.shift), WAVES * (dtype == JOLT_BF16 ? 32 : 16));
   const int64_t whole = (int64_t)a.n_req * a.heads;    // workgroups that takes
   if (most <= 32 && steps <= 3 && steps * ceil_div(whole, BLOCKS / 2) <= 4) {
@@ -1121,7 +1133,7 @@ PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype) {
   }
   if (a.T > 0) {
     // Up to 32 rows few() reads the prefix at the rate of memory: 32 rows on 32768 tokens of 8 heads
-    // take 38 us, 44 by many(); 17 rows on 4001 tokens of 40 heads 29 and 32.
+    // take 31 us, 33 by many(); 17 rows on 4001 tokens of 40 heads 25 and 24.
     c.prefix_few = rows <= 32;
     if (c.prefix_few) {
       c.prefix_nq = rows <= 16 ? 1 : 2;
@@ -1142,7 +1154,8 @@ PrefixCut prefix_attend_cut(const PrefixAttendArgs &a, int d, int dtype) {
   c.limit = 0x7fffffff;
   if (a.max_pages > 0) {
     // Requests of up to 32 rows by few(), also where that takes two groups of rows a wave: 64 requests
-    // of up to 32 rows and 500 tokens take 22 us, 26 with those past 16 rows by many() (fp32 33, 64).
+    // of up to 32 rows and 100 to 500 tokens take 31 us, 32 with those past 16 rows by many() (fp32 57
+    // and 74).
     c.few_nq = most <= 16 ? 1 : 2;
     c.limit = 16 * c.few_nq;
     c.few_rows = (int)std::min<int64_t>(most, c.limit);

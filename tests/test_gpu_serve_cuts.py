@@ -1,6 +1,6 @@
 """GPU tests of jolt_prefix_attend over calls that run each of its kernels' forms (serve_cuts.py):
-random inputs against the definition in float64, with the tolerances of test_gpu_serve.py, and
-equal weights over values of which every one counts.
+random inputs against the definition in float64, with the tolerances of test_gpu_serve.py, equal
+weights over values of which every one counts, and values that show the weights themselves.
 """
 import numpy as np
 import pytest
@@ -113,3 +113,50 @@ def test_requests_that_share_pages(new, T):
     for x in (b.tk, b.tv):
         x[2][:, 24:32] = x[2][:, 8:16]
     b.check(b.run(max_new=max(new)), want64(b))
+
+
+def _weights_seen(b, where):
+    """Values that make an output a row's weights themselves: the unit rows for the d tokens of the prefix
+    (where = "prefix") or for the first d tokens of every tail, zero for all others."""
+    eye = torch.eye(b.d, device="cuda", dtype=b.V.dtype)
+    b.V.zero_()
+    if where == "prefix":
+        b.V[1, :, :b.d] = eye
+    columns = torch.as_tensor(b.table, device="cuda").clamp(min=0).long()
+    for r, v in enumerate(b.tv):
+        v.zero_()
+        if where == "tails":
+            v[:, :b.d] = eye[:v.shape[1]]
+        x = torch.arange(v.shape[1], device="cuda")
+        b.Vp[columns[r, x // b.page], :, x % b.page] = v.transpose(0, 1)
+
+
+@pytest.mark.parametrize("where", ["prefix", "tails"])
+@pytest.mark.parametrize("new,columns", [([1, 1], 0), ([1, 1], 64), ([3, 2], 64), ([40, 2], 0)])
+def test_bf16_weights_keep_sixteen_bits(where, new, columns):
+    """With values that show the weights every entry is off by the rounding of the output (half a step)
+    and by its weight alone: two bf16 terms, the second below 2^-7 of the weight and rounded at
+    2^-8 of itself; scores and sums as in test_gpu_serve.py."""
+    d = 64
+    b = Batch("bf16", d, [d, 9], new, 2, 4, d, 16, seed=3)
+    b.table = np.pad(b.table, ((0, 0), (0, max(0, columns - b.table.shape[1]))), constant_values=-1)
+    _weights_seen(b, where)
+    O, lse = b.run(max_new=max(new))
+    want, wl, A, S = want64(b)
+    ds = (d + 4) * 2.0 ** -24 * S + 2.0 ** -22 * (np.abs(wl) + S)
+    w = 2 * ds + (b.T + b.kv_len.max() + 8) * 2.0 ** -24 + 2.0 ** -15 + 2.0 ** -23
+    assert (want > 0).any() and (np.abs(O - want) <= (2.0 ** -8 + w[..., None]) * want).all()
+
+
+@pytest.mark.parametrize("new,T", [([1, 1], 50), ([1, 1], 600), ([40, 2], 600)])
+def test_infinite_value_under_weights_of_one_bit(new, T):
+    """Equal weights, which one bf16 term holds exactly: an infinite value stays infinite, of its sign."""
+    b = Batch("bf16", T, [60, 5], new, 2, 4, 64, 16)
+    b.Q.zero_()
+    b.V[1, 1, 7, 3], b.V[1, 0, 9, 5] = float("inf"), -float("inf")
+    b.Vp[b.table[0, 0], 0, 2, 6] = float("inf")
+    O, _ = b.run(max_new=max(new))
+    n0 = int(b.q_start[1])
+    assert np.isposinf(O[:, 4:, 3]).all() and np.isneginf(O[:, :4, 5]).all() and np.isposinf(O[:n0, :4, 6]).all()
+    for x, f in ((O[:n0, 4:], [3]), (O[:n0, :4], [5, 6]), (O[n0:, :4], [5])):
+        assert np.isfinite(np.delete(x, f, 2)).all()
