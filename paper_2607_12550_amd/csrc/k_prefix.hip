@@ -293,8 +293,8 @@ struct Rows {
   // o += V^T P^T for 16 SUBS tokens whose values stand in LDS.  For the bf16 product (values are
   // bf16 already) a weight is the sum of two bf16 terms, its upper half and the rest, right to 2^-15: the
   // output's error is that of its own rounding.  One term, the weight rounded, makes it 1.2 .. 1.4
-  // times that, and takes 196 us for 256 requests on 32768 tokens, not 228, and 115 for 1025 prompt
-  // rows on 4096, not 135; calls that memory bounds take the same (64 requests on 4096 tokens 24.3 us).
+  // times that, and takes 196 us for 256 requests on 32768 tokens, not 224, and 115 for 1025 prompt
+  // rows on 4096, not 133; calls that memory bounds take the same (64 requests on 4096 tokens 24.3 us).
   // ABOVE_ONE adds 2^-23 of the weight to the rest, so that it is above zero wherever the weight is and
   // times an infinite value no NaN.
   static constexpr float ABOVE_ONE = 1.f + 0x1p-23f;
